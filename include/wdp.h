@@ -1,0 +1,241 @@
+/*
+ * wdp.h — C ABI of libwd for the POLICY's side of the roll-out loop on one MI355X.
+ *
+ * wd.h and wdc.h draw actions from the probabilities that a policy answers with, step the
+ * environments and record the batch that the policy trains on (arXiv 2108.13976, Sec. 4.5
+ * items 3-7).  The operators here are what a policy needs on the other side of those calls:
+ * its evaluation for every agent of every iteration (a norm with the residual's addition and
+ * an 8-bit output, the 8-bit matrix product that reads it), the verification of actions or
+ * tokens that a cheaper policy drafted (beside wd_sample: the drafts become draws from the
+ * present policy), and the update of its weights (AdamW).  The paper leaves policy and
+ * trainer to the deep-learning framework; formulas, layouts and roundings are this build's
+ * own and stated here, operator by operator.
+ *
+ * Conventions are those of wd.h where they apply:
+ *   - Every function returns WD_OK (0) or a negative wd_status; none throws or aborts.  On
+ *     failure nothing has been enqueued, with one exception: WD_E_HIP from a call of several
+ *     launches can follow after some of them.
+ *   - Each call gets a config (sizes, types, strides, stream) and a struct of pointers, as
+ *     wd_iterate_static does; there is no handle, nothing is kept between calls and nothing is
+ *     allocated.  Calls may come from several threads and run on several streams at once.
+ *   - All pointers in the buffer structs are DEVICE pointers, owned by the caller; configs and
+ *     structs are HOST memory and may be freed when the call returns.  Kernels run on
+ *     config.stream (hipStream_t, borrowed; NULL = the default stream) of the CURRENT device
+ *     and are not synchronised.  Everything here can be captured into a HIP graph (kernels
+ *     only; no fills or copies).
+ *   - Workspaces are the caller's: the wdp_*_workspace function says how many bytes a config
+ *     needs (0: the pointer may be NULL).  They carry nothing from call to call and need no
+ *     initial value; two calls that can overlap in time need two.  256-byte aligned.
+ *   - Alignment: a pointer is aligned to its element (8-bit: 1 byte).  Rows that start at
+ *     16-byte boundaries (base and strides) run faster, results do not depend on it.
+ *   - Strides are in elements and count from row to row; they are >= the row's length (a
+ *     stride of one row only is not looked at).  Elements of a row are adjacent.
+ *   - Outputs do not overlap inputs unless it says so.  Bytes of a row beyond its length,
+ *     and rows beyond the last, are neither read into a result nor written.
+ *   - Zero rows (or sequences, or tensors) are a valid call that does nothing.
+ *
+ * 8-bit formats: E4M3 is the finite-only format (bias 7, largest 448, one NaN per sign, no
+ * infinity), E5M2 the IEEE-like one (bias 15, largest 57344, infinities); rounding is to
+ * nearest, ties to even.
+ */
+#ifndef WDP_H
+#define WDP_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "wd.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum wdp_type { WDP_F32 = 0, WDP_BF16 = 1, WDP_F16 = 2, WDP_E4M3 = 3, WDP_E5M2 = 4 } wdp_type;
+
+#define WDP_BLOCK 128 /* elements of a row that share a scale */
+
+/* ---- norm -------------------------------------------------------------------------------
+ * Row m of `width` elements, in float32 from the stored values on:
+ *   h    = x + residual, rounded to `type`  (residual NULL: h = x)
+ *   rstd = 1 / sqrt(mean(h * h) + eps)
+ *   y    = h * rstd * weight
+ * and, with q given, per block of 128 elements of the row (the last may be shorter)
+ *   scale = max(max |y|, 2^-100) / largest(q_type),   q = round(y / scale)
+ * from the unrounded y.  The product of wdp_product reads q and scale as they stand.  A NaN
+ * in a row makes the whole row NaN (q, scale, y, rstd), an infinity makes it NaN where it
+ * stands and zero elsewhere; other rows are untouched by either.
+ * Each of h, y, q + scale, rstd is written if its pointer is given (q and scale go together,
+ * one of the four at least).  h may be x or residual (in place, with the same stride). */
+typedef struct wdp_norm_config {
+  uint32_t struct_size;   /* = sizeof(wdp_norm_config); ABI check                          */
+  int32_t type;           /* of x, residual, h, y, dy, dh, dx: WDP_F32, WDP_BF16, WDP_F16  */
+  int32_t weight_type;    /* WDP_F32 or `type`                                             */
+  int32_t q_type;         /* WDP_E4M3 or WDP_E5M2 (looked at only if q is given)           */
+  int64_t rows;           /* >= 0                                                          */
+  int32_t width;          /* 1 .. 32768                                                    */
+  float eps;              /* >= 0, finite                                                  */
+  int64_t x_stride, residual_stride, h_stride, y_stride;
+  int64_t q_stride;
+  int64_t scale_row_stride, scale_block_stride; /* scale of row m, block b at m * row + b * block */
+  int64_t dy_stride, dh_stride, dx_stride;      /* backward only                           */
+  void* stream;
+} wdp_norm_config;
+
+typedef struct wdp_norm_buffers {
+  const void* x;
+  const void* residual; /* or NULL                                                        */
+  const void* weight;   /* [width], or NULL: ones                                         */
+  void* h;
+  void* y;
+  void* q;
+  float* scale;
+  float* rstd;          /* [rows]                                                         */
+} wdp_norm_buffers;
+
+int wdp_norm(const wdp_norm_config* cfg, const wdp_norm_buffers* bufs);
+
+/* The norm's gradients, from h and rstd as wdp_norm wrote them:
+ *   xhat = h * rstd,  g = dy * weight
+ *   dx = dh + rstd * (g - xhat * mean(g * xhat))      (dh NULL: without it), rounded to `type`
+ *   dw = sum over rows of dy * xhat                   (float32, [width])
+ * dx is the gradient of x and of residual alike.  dy is y's gradient, dh what reaches h on
+ * other ways.  dw NULL: not wanted.  dx NULL: only dw is wanted.  dx may be dy or dh (in
+ * place, with the same stride).  dw is the same for the same inputs in every run: partial
+ * sums in the workspace, joined in a fixed order. */
+typedef struct wdp_norm_grad_buffers {
+  const void* dy;
+  const void* dh;
+  const void* h;
+  const void* weight;
+  const float* rstd;
+  void* dx;
+  float* dw;
+  void* workspace;
+} wdp_norm_grad_buffers;
+
+int wdp_norm_backward_workspace(const wdp_norm_config* cfg, size_t* bytes);
+int wdp_norm_backward(const wdp_norm_config* cfg, const wdp_norm_grad_buffers* bufs);
+
+/* ---- 8-bit product ------------------------------------------------------------------------
+ *   c[i][j] = sum over blocks b of 128 along k:
+ *               a_scale[i][b] * b_scale[j / 128 or j][b] * sum over k in b of a[i][k] * b[j][k]
+ * a is [m][k], b is [n][k] (a layer's weights as rows of outputs), both 8-bit; c is [m][n].
+ * The sums within a block and over the blocks are float32, c is rounded once.  A NaN code or scale reaches the elements of its row or column. */
+typedef struct wdp_product_config {
+  uint32_t struct_size;   /* = sizeof(wdp_product_config)                                   */
+  int32_t a_type, b_type; /* WDP_E4M3 or WDP_E5M2                                           */
+  int32_t c_type;         /* WDP_F32, WDP_BF16, WDP_F16                                     */
+  int64_t m;              /* 0 .. 2^31 - 1                                                  */
+  int32_t n;              /* 0 .. 2^24                                                      */
+  int32_t k;              /* 1 .. 2^24                                                      */
+  int32_t b_scale_rows;   /* rows of b that share a scale: 128 or 1                         */
+  int64_t a_stride, b_stride, c_stride;
+  int64_t a_scale_row_stride, a_scale_block_stride;
+  int64_t b_scale_row_stride, b_scale_block_stride; /* row: of b, or of its groups of 128   */
+  void* stream;
+} wdp_product_config;
+
+typedef struct wdp_product_buffers {
+  const void* a;
+  const float* a_scale;
+  const void* b;
+  const float* b_scale;
+  void* c;
+  void* workspace;
+} wdp_product_buffers;
+
+int wdp_product_workspace(const wdp_product_config* cfg, size_t* bytes);
+int wdp_product(const wdp_product_config* cfg, const wdp_product_buffers* bufs);
+
+/* ---- verification of drafts ----------------------------------------------------------------
+ * A sequence has n drafted tokens x_0 .. x_{n-1} (n = lengths[s], clamped to [0, drafts]; lengths
+ * NULL: n = drafts), drawn from the rows q_i of `draft_probs`, the rows p_i of `target` and
+ * drafts + 1 uniform numbers u in [0, 1).
+ *   - x_i is accepted while u_i * q_i(x_i) < p_i(x_i) (both sides exact in float64); the first
+ *     that is not, and a token outside [0, vocab), ends it.  a = how many were accepted.
+ *   - a < n: a token is drawn with u_drafts from r = max(p_a - q_a, 0);
+ *     a = n and bonus: from r = max(p_n, 0);  a = n without bonus: no draw.
+ *     The draw is the smallest j with r_j > 0 and r_0 + .. + r_j > u * sum(r) (float64), or the last
+ *     j with r_j > 0 if none is.  Where no r_j > 0, r = max(p, 0) takes its place; where that
+ *     is empty too, the token is vocab - 1.  NaN counts as zero.
+ *   - tokens[s] = x_0 .. x_{a-1}, then the drawn token, then -1; accepted[s] = a.
+ * So that whatever q drafted, the tokens are draws from p.  Probabilities need not be
+ * normalised.  target is [batch][drafts + bonus][vocab], draft_probs [batch][drafts][vocab],
+ * drafts_in [batch][drafts], u [batch][drafts + 1], tokens [batch][drafts + bonus]
+ * (contiguous but for the two probability arrays).  tokens may be drafts_in if bonus = 0 (in
+ * place: the drafted actions of wd_sample become verified ones).  accepted may be NULL. */
+typedef struct wdp_verify_config {
+  uint32_t struct_size;   /* = sizeof(wdp_verify_config)                                     */
+  int32_t type;           /* of the probabilities: WDP_F32, WDP_BF16, WDP_F16                */
+  int64_t batch;          /* 0 .. 2^31 - 1                                                   */
+  int32_t drafts;         /* 0 .. 64; 0 only with bonus                                      */
+  int32_t vocab;          /* 1 .. 2^24                                                       */
+  int32_t bonus;          /* 0 or 1: target has a row behind the last draft                  */
+  int64_t target_batch_stride, target_row_stride;
+  int64_t draft_batch_stride, draft_row_stride;
+  void* stream;
+} wdp_verify_config;
+
+typedef struct wdp_verify_buffers {
+  const void* target;
+  const void* draft_probs;  /* may be NULL if drafts = 0, like drafts_in                     */
+  const int32_t* drafts_in;
+  const int32_t* lengths;
+  const float* u;
+  int32_t* accepted;
+  int32_t* tokens;
+  void* workspace;
+} wdp_verify_buffers;
+
+int wdp_verify_workspace(const wdp_verify_config* cfg, size_t* bytes);
+int wdp_verify(const wdp_verify_config* cfg, const wdp_verify_buffers* bufs);
+
+/* ---- AdamW --------------------------------------------------------------------------------
+ * One step over `count` tensors at once.  Per element, in float32 (the constants made from the
+ * config in float64 and rounded once), with g = grad * grad_scale:
+ *   m = beta1 * m + (1 - beta1) * g
+ *   v = beta2 * v + (1 - beta2) * g * g
+ *   p = p * (1 - lr * weight_decay) - lr * (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * p is `master` (float32) if it is given, else `param`; param = p rounded to its type.
+ * state_bits 32: exp_avg and exp_avg_sq hold m and v in float32.
+ * state_bits 8: exp_avg holds m, exp_avg_sq the ROOT s = sqrt(v), both as E4M3 with a float32
+ * scale for each block of 128 elements of the tensor (avg_scale, sq_scale: [ceil(numel / 128)]);
+ * scale = max(max |.|, 2^-100) / 448 of the new values.  The update of p uses the new m and v
+ * before they are rounded.  They are rounded up or down at random, with probabilities that
+ * leave the mean unchanged (to nearest, a change of 1 - beta2 per step is less than half a
+ * code's step and the state would stand still): v / step(v) + r, downwards, with r the low
+ * (m) or high (s) 16 bits / 65536 of word e mod 4 of the random block of (seed; e / 4, step,
+ * stream 4), where e numbers the elements of the call: 128 * (blocks of the tensors before)
+ * + the place in the tensor.  A root above zero does not become zero.
+ * A NaN or an infinity in a gradient reaches its element, with 8 bits also its block. */
+typedef struct wdp_adamw_config {
+  uint32_t struct_size;      /* = sizeof(wdp_adamw_config)                                   */
+  int32_t state_bits;        /* 32 or 8                                                      */
+  double lr, beta1, beta2, eps, weight_decay; /* finite; lr, eps, weight_decay >= 0, betas in [0, 1) */
+  int64_t step;              /* >= 1: number of this step, if step_device is NULL            */
+  const int64_t* step_device;/* DEVICE, or NULL: the number is read when the kernel runs (a captured
+                                step that a caller's kernel counts up); below 1 counts as 1  */
+  const float* grad_scale;   /* DEVICE, or NULL: 1                                           */
+  uint64_t seed;             /* state_bits 8                                                 */
+  void* stream;
+} wdp_adamw_config;
+
+typedef struct wdp_adamw_tensor {
+  void* param;
+  const void* grad;
+  float* master;       /* or NULL                                                             */
+  void* exp_avg;
+  void* exp_avg_sq;
+  float* avg_scale;    /* state_bits 8, else NULL                                             */
+  float* sq_scale;
+  int64_t numel;       /* >= 0                                                                */
+  int32_t param_type;  /* WDP_F32, WDP_BF16, WDP_F16                                          */
+  int32_t grad_type;   /* WDP_F32 or param_type                                               */
+} wdp_adamw_tensor;
+
+int wdp_adamw(const wdp_adamw_config* cfg, const wdp_adamw_tensor* tensors, int count);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* WDP_H */

@@ -8,7 +8,8 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = [os.path.join(CSRC, "wd_api.hip"), os.path.join(CSRC, "wd_kernels.hip"), os.path.join(CSRC, "wdc.hip")]
+SOURCES = [os.path.join(CSRC, name + ".hip") for name in
+           ("wd_api", "wd_kernels", "wdc", "wdp_norm", "wdp_product", "wdp_verify", "wdp_adamw")]
 LIBRARY = os.path.join(HERE, "libwd.so")
 
 HIPCC_FLAGS = [

@@ -1,0 +1,264 @@
+// wdp_adamw.hip — one AdamW step over many tensors at once, states in 32 or 8 bits (include/wdp.h: wdp_adamw).
+//
+// The step reads and writes every weight and both states once and computes about twenty operations an element on the
+// way: memory bounds it, and for a small policy the launches do.  So the tensors travel in the kernel's arguments (48
+// at a time: nothing to copy to the device before the launch, nothing to keep alive behind it, and a captured step
+// holds its own), and a workgroup finds its tensor with one compare a lane over the tensors' first pieces.
+#include "wdp_common.h"
+
+namespace wdp {
+namespace {
+
+constexpr int kMaxTensors = 48;
+constexpr int kVec = 8, kThreads = 256, kPiece = kThreads * kVec;  // elements of a workgroup
+
+struct Tensor {
+  void* param;
+  const void* grad;
+  float* master;
+  void *exp_avg, *exp_avg_sq;
+  float *avg_scale, *sq_scale;
+  int64_t numel;
+};
+
+struct AdamArgs {
+  Tensor t[kMaxTensors];
+  uint32_t first[kMaxTensors];   // the tensor's first workgroup of the launch
+  uint32_t number[kMaxTensors];  // its first block of 128 in the call's numbering
+  const int64_t* step_device;
+  const float* grad_scale;
+  int64_t step;
+  double beta1, beta2, lr;
+  float b1, b2, rest1, rest2, decay, eps;
+  float c1, c2;  // lr / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
+  uint32_t seed_lo, seed_hi;
+  int32_t count;
+};
+static_assert(sizeof(AdamArgs) <= 4096, "a launch's arguments");
+
+// Random numbers: Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC'11), as the sampler's.
+__device__ __forceinline__ void philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1, uint32_t w[4]) {
+#pragma unroll
+  for (int round = 0; round < 10; ++round) {
+    const uint32_t hi_a = __umulhi(0xD2511F53u, c0), lo_a = 0xD2511F53u * c0;
+    const uint32_t hi_b = __umulhi(0xCD9E8D57u, c2), lo_b = 0xCD9E8D57u * c2;
+    c0 = hi_b ^ c1 ^ k0;
+    c1 = lo_b;
+    c2 = hi_a ^ c3 ^ k1;
+    c3 = lo_a;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
+}
+
+// v (its size at most 448, or NaN) to a neighbour in E4M3, by 16 random bits: in units of the code's step at v,
+// plus a fraction, downwards.  Exact in float32 but for the sum's last bit.
+__device__ __forceinline__ float round_at_random(float v, uint32_t bits) {
+  const float size = fabsf(v);
+  const uint32_t exponent = __float_as_uint(fmaxf(size, 0.015625f)) & 0x7F800000u;  // of the larger of size and 2^-6
+  const float step = __uint_as_float(exponent - (3u << 23)), per = __uint_as_float(0x7F000000u - exponent + (3u << 23));
+  const float q = fminf(floorf(size * per + float(bits) * (1.0f / 65536.0f)) * step, 448.0f);
+  return v != v ? v : copysignf(q, v);
+}
+
+__device__ __forceinline__ void from_codes(const uint8_t* p, int n, float v[kVec]) {
+  uint32_t lo = 0, hi = 0;
+  if (n >= kVec) {
+    struct __attribute__((packed, aligned(1))) Codes {
+      uint32_t lo, hi;
+    };
+    const Codes c = *reinterpret_cast<const Codes*>(p);
+    lo = c.lo, hi = c.hi;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (i < n) (i < 4 ? lo : hi) |= uint32_t(p[i]) << (8 * (i & 3));
+  }
+  v[0] = __builtin_amdgcn_cvt_f32_fp8(lo, 0), v[1] = __builtin_amdgcn_cvt_f32_fp8(lo, 1);
+  v[2] = __builtin_amdgcn_cvt_f32_fp8(lo, 2), v[3] = __builtin_amdgcn_cvt_f32_fp8(lo, 3);
+  v[4] = __builtin_amdgcn_cvt_f32_fp8(hi, 0), v[5] = __builtin_amdgcn_cvt_f32_fp8(hi, 1);
+  v[6] = __builtin_amdgcn_cvt_f32_fp8(hi, 2), v[7] = __builtin_amdgcn_cvt_f32_fp8(hi, 3);
+}
+
+__device__ __forceinline__ void write_codes(uint8_t* p, int n, const float v[kVec]) {
+  const uint32_t lo = to_codes(WDP_E4M3, v[0], v[1], v[2], v[3]), hi = to_codes(WDP_E4M3, v[4], v[5], v[6], v[7]);
+  if (n >= kVec) {
+    struct __attribute__((packed, aligned(1))) Codes {
+      uint32_t lo, hi;
+    };
+    *reinterpret_cast<Codes*>(p) = Codes{lo, hi};
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (i < n) p[i] = uint8_t((i < 4 ? lo >> (8 * i) : hi >> (8 * (i - 4))) & 0xFF);
+  }
+}
+
+template <typename P, typename G, bool EIGHT> __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamArgs a) {
+  // the last tensor whose first workgroup is not behind this one
+  const int lane = threadIdx.x & 63;
+  const bool reached = lane < a.count && a.first[lane < kMaxTensors ? lane : 0] <= blockIdx.x;
+  const int which = __builtin_amdgcn_readfirstlane(__popcll(__ballot(reached)) - 1);
+  const Tensor t = a.t[which];
+  const int64_t at = int64_t(blockIdx.x - a.first[which]) * kPiece + threadIdx.x * kVec;
+  int64_t step = a.step;
+  float c1 = a.c1, c2 = a.c2;
+  if (a.step_device) {
+    step = *a.step_device;
+    if (step < 1) step = 1;
+    c1 = float(a.lr / (1.0 - pow(a.beta1, double(step))));
+    c2 = float(sqrt(1.0 / (1.0 - pow(a.beta2, double(step)))));
+  }
+  const float gscale = a.grad_scale ? *a.grad_scale : 1.0f;
+  const int n = t.numel - at >= kVec ? kVec : t.numel > at ? int(t.numel - at) : 0;
+  float p[kVec], g[kVec], m[kVec], v[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) p[i] = g[i] = m[i] = v[i] = 0.0f;
+  if (n) {
+    if (t.master) load_some<float, kVec>(t.master + at, n, p);
+    else load_some<P, kVec>(static_cast<const P*>(t.param) + at, n, p);
+    load_some<G, kVec>(static_cast<const G*>(t.grad) + at, n, g);
+    if (EIGHT) {
+      from_codes(static_cast<const uint8_t*>(t.exp_avg) + at, n, m);
+      from_codes(static_cast<const uint8_t*>(t.exp_avg_sq) + at, n, v);
+      const float ms = t.avg_scale[at / WDP_BLOCK], vs = t.sq_scale[at / WDP_BLOCK];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        m[i] *= ms;
+        v[i] *= vs;
+        v[i] *= v[i];
+      }
+    } else {
+      load_some<float, kVec>(static_cast<const float*>(t.exp_avg) + at, n, m);
+      load_some<float, kVec>(static_cast<const float*>(t.exp_avg_sq) + at, n, v);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    g[i] *= gscale;
+    m[i] = a.b1 * m[i] + a.rest1 * g[i];
+    v[i] = a.b2 * v[i] + a.rest2 * g[i] * g[i];
+    p[i] = p[i] * a.decay - c1 * m[i] / (sqrtf(v[i]) * c2 + a.eps);
+  }
+  if (n) {
+    if (t.master) store_some<float, kVec>(t.master + at, n, p);
+    store_some<P, kVec>(static_cast<P*>(t.param) + at, n, p);
+    if (!EIGHT) {
+      store_some<float, kVec>(static_cast<float*>(t.exp_avg) + at, n, m);
+      store_some<float, kVec>(static_cast<float*>(t.exp_avg_sq) + at, n, v);
+    }
+  }
+  if (EIGHT) {
+    float most_m = 0.0f, most_s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      if (i >= n) m[i] = v[i] = 0.0f;
+      v[i] = sqrtf(v[i]);
+      most_m = fmaxf(most_m, fabsf(m[i]));
+      most_s = fmaxf(most_s, v[i]);
+    }
+    const float ms = fmaxf(group_max<16>(most_m), kTiny) / kLargestE4M3, vs = fmaxf(group_max<16>(most_s), kTiny) / kLargestE4M3;
+    if (n) {
+      const uint64_t block = a.number[which] + uint64_t(at / WDP_BLOCK);
+      const uint64_t four = block * (WDP_BLOCK / 4) + (at % WDP_BLOCK) / 4;
+      uint32_t w[kVec];
+      const uint32_t stream = 4u | uint32_t(uint64_t(step) >> 32) << 8;
+      philox(uint32_t(four), uint32_t(four >> 32), uint32_t(step), stream, a.seed_lo, a.seed_hi, w);
+      philox(uint32_t(four + 1), uint32_t((four + 1) >> 32), uint32_t(step), stream, a.seed_lo, a.seed_hi, w + 4);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const bool some = v[i] > 0.0f;
+        m[i] = round_at_random(m[i] / ms, w[i] & 0xFFFFu);
+        v[i] = round_at_random(v[i] / vs, w[i] >> 16);
+        if (some) v[i] = fmaxf(v[i], 0.001953125f);  // 2^-9, the least code: the step that follows divides by it
+      }
+      write_codes(static_cast<uint8_t*>(t.exp_avg) + at, n, m);
+      write_codes(static_cast<uint8_t*>(t.exp_avg_sq) + at, n, v);
+      if (at % WDP_BLOCK == 0) {
+        t.avg_scale[at / WDP_BLOCK] = ms;
+        t.sq_scale[at / WDP_BLOCK] = vs;
+      }
+    }
+  }
+}
+
+template <typename P, typename G> void launch_types(const AdamArgs& a, bool eight, unsigned blocks, hipStream_t stream) {
+  if (eight) adamw_kernel<P, G, true><<<dim3(blocks), dim3(kThreads), 0, stream>>>(a);
+  else adamw_kernel<P, G, false><<<dim3(blocks), dim3(kThreads), 0, stream>>>(a);
+}
+void launch(int param, int grad, const AdamArgs& a, bool eight, unsigned blocks, hipStream_t stream) {
+  if (param == WDP_F32) launch_types<float, float>(a, eight, blocks, stream);
+  else if (param == WDP_BF16 && grad == WDP_F32) launch_types<bf16, float>(a, eight, blocks, stream);
+  else if (param == WDP_BF16) launch_types<bf16, bf16>(a, eight, blocks, stream);
+  else if (grad == WDP_F32) launch_types<f16, float>(a, eight, blocks, stream);
+  else launch_types<f16, f16>(a, eight, blocks, stream);
+}
+
+bool amount(double v) { return v >= 0.0 && isfinite(v); }
+
+}  // namespace
+}  // namespace wdp
+
+extern "C" int wdp_adamw(const wdp_adamw_config* cfg, const wdp_adamw_tensor* tensors, int count) {
+  using namespace wdp;
+  if (!cfg) return WD_E_NULL;
+  if (cfg->struct_size != sizeof(wdp_adamw_config) || (cfg->state_bits != 32 && cfg->state_bits != 8) || count < 0) return WD_E_CONFIG;
+  if (!amount(cfg->lr) || !amount(cfg->eps) || !amount(cfg->weight_decay) || !(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) ||
+      !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || (!cfg->step_device && cfg->step < 1))
+    return WD_E_CONFIG;
+  if (!aligned(cfg->step_device, 8) || !aligned(cfg->grad_scale, 4)) return WD_E_ALIGN;
+  if (count == 0) return WD_OK;
+  if (!tensors) return WD_E_NULL;
+  const bool eight = cfg->state_bits == 8;
+  uint64_t all = 0;
+  for (int i = 0; i < count; ++i) {
+    const wdp_adamw_tensor& t = tensors[i];
+    if (t.numel < 0 || t.numel > (int64_t(1) << 38) || !is_float_type(t.param_type) || (t.grad_type != WDP_F32 && t.grad_type != t.param_type)) return WD_E_CONFIG;
+    all += uint64_t((t.numel + WDP_BLOCK - 1) / WDP_BLOCK);
+    if (all > 0xFFFFFFFFu) return WD_E_UNSUPPORTED;  // (2^39 elements in a call)
+    if (t.numel == 0) continue;
+    if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (eight && (!t.avg_scale || !t.sq_scale))) return WD_E_NULL;
+    const size_t e = size_of(t.param_type), s = eight ? 1 : 4;
+    if (!aligned(t.param, e) || !aligned(t.grad, size_of(t.grad_type)) || !aligned(t.master, 4) || !aligned(t.exp_avg, s) || !aligned(t.exp_avg_sq, s) ||
+        !aligned(t.avg_scale, 4) || !aligned(t.sq_scale, 4))
+      return WD_E_ALIGN;
+  }
+  AdamArgs a;
+  a.step_device = cfg->step_device;
+  a.grad_scale = cfg->grad_scale;
+  a.step = cfg->step;
+  a.beta1 = cfg->beta1, a.beta2 = cfg->beta2, a.lr = cfg->lr;
+  a.b1 = float(cfg->beta1), a.b2 = float(cfg->beta2), a.rest1 = float(1.0 - cfg->beta1), a.rest2 = float(1.0 - cfg->beta2);
+  a.decay = float(1.0 - cfg->lr * cfg->weight_decay), a.eps = float(cfg->eps);
+  a.c1 = a.c2 = 0.0f;
+  if (!cfg->step_device) {
+    a.c1 = float(cfg->lr / (1.0 - pow(cfg->beta1, double(cfg->step))));
+    a.c2 = float(sqrt(1.0 / (1.0 - pow(cfg->beta2, double(cfg->step)))));
+  }
+  a.seed_lo = uint32_t(cfg->seed), a.seed_hi = uint32_t(cfg->seed >> 32);
+  // launches of up to 48 neighbouring tensors of the same types
+  uint32_t number = 0;
+  for (int i = 0; i < count;) {
+    const int param = tensors[i].param_type, grad = tensors[i].grad_type;
+    uint64_t blocks = 0;
+    a.count = 0;
+    for (; i < count && a.count < kMaxTensors; ++i) {
+      const wdp_adamw_tensor& t = tensors[i];
+      if (t.numel == 0) continue;
+      const uint64_t more = uint64_t((t.numel + kPiece - 1) / kPiece);
+      if (t.param_type != param || t.grad_type != grad || blocks + more > 0x7FFFFFFFu) break;
+      a.t[a.count] = Tensor{t.param, t.grad, t.master, t.exp_avg, t.exp_avg_sq, t.avg_scale, t.sq_scale, t.numel};
+      a.first[a.count] = uint32_t(blocks);
+      a.number[a.count] = number;
+      number += uint32_t((t.numel + WDP_BLOCK - 1) / WDP_BLOCK);
+      blocks += more;
+      ++a.count;
+    }
+    if (blocks == 0) continue;
+    launch(param, grad, a, eight, unsigned(blocks), static_cast<hipStream_t>(cfg->stream));
+    const int status = launched();
+    if (status != WD_OK) return status;
+  }
+  return WD_OK;
+}

@@ -1,0 +1,466 @@
+"""The policy's side of the roll-out loop (``include/wdp.h``): norm, 8-bit product, verification of drafts, AdamW.
+
+First the C ABI, one Python function per entry point; then functions on torch tensors, which check their arguments,
+allocate outputs and workspaces and run on the tensors' device, on its current stream.  Every step runs in libwd's HIP
+kernels; without a GPU the tensor functions raise.
+"""
+import collections
+import ctypes
+
+from . import binding
+from .binding import WD_OK, WdError, load_library
+
+WDP_F32, WDP_BF16, WDP_F16, WDP_E4M3, WDP_E5M2 = range(5)
+WDP_BLOCK = 128
+
+
+def _structure(name, *fields):
+    kinds = {"u4": ctypes.c_uint32, "i4": ctypes.c_int32, "i8": ctypes.c_int64, "u8": ctypes.c_uint64, "f4": ctypes.c_float,
+             "f8": ctypes.c_double, "p": ctypes.c_void_p}
+    return type(name, (ctypes.Structure,), {"_fields_": [(n, kinds[k]) for k, names in fields for n in names.split()]})
+
+
+wdp_norm_config = _structure(
+    "wdp_norm_config", ("u4", "struct_size"), ("i4", "type weight_type q_type"), ("i8", "rows"), ("i4", "width"), ("f4", "eps"),
+    ("i8", "x_stride residual_stride h_stride y_stride q_stride scale_row_stride scale_block_stride dy_stride dh_stride dx_stride"),
+    ("p", "stream"))
+wdp_norm_buffers = _structure("wdp_norm_buffers", ("p", "x residual weight h y q scale rstd"))
+wdp_norm_grad_buffers = _structure("wdp_norm_grad_buffers", ("p", "dy dh h weight rstd dx dw workspace"))
+wdp_product_config = _structure(
+    "wdp_product_config", ("u4", "struct_size"), ("i4", "a_type b_type c_type"), ("i8", "m"), ("i4", "n k b_scale_rows"),
+    ("i8", "a_stride b_stride c_stride a_scale_row_stride a_scale_block_stride b_scale_row_stride b_scale_block_stride"), ("p", "stream"))
+wdp_product_buffers = _structure("wdp_product_buffers", ("p", "a a_scale b b_scale c workspace"))
+wdp_verify_config = _structure(
+    "wdp_verify_config", ("u4", "struct_size"), ("i4", "type"), ("i8", "batch"), ("i4", "drafts vocab bonus"),
+    ("i8", "target_batch_stride target_row_stride draft_batch_stride draft_row_stride"), ("p", "stream"))
+wdp_verify_buffers = _structure("wdp_verify_buffers", ("p", "target draft_probs drafts_in lengths u accepted tokens workspace"))
+wdp_adamw_config = _structure(
+    "wdp_adamw_config", ("u4", "struct_size"), ("i4", "state_bits"), ("f8", "lr beta1 beta2 eps weight_decay"), ("i8", "step"),
+    ("p", "step_device grad_scale"), ("u8", "seed"), ("p", "stream"))
+wdp_adamw_tensor = _structure(
+    "wdp_adamw_tensor", ("p", "param grad master exp_avg exp_avg_sq avg_scale sq_scale"), ("i8", "numel"), ("i4", "param_type grad_type"))
+
+_declared = None
+
+
+def _library():
+    global _declared
+    if _declared is None:
+        lib = load_library()
+        size = ctypes.POINTER(ctypes.c_size_t)
+        for name, config, buffers in (("wdp_norm", wdp_norm_config, wdp_norm_buffers),
+                                      ("wdp_norm_backward", wdp_norm_config, wdp_norm_grad_buffers),
+                                      ("wdp_product", wdp_product_config, wdp_product_buffers),
+                                      ("wdp_verify", wdp_verify_config, wdp_verify_buffers)):
+            call = getattr(lib, name)
+            call.argtypes, call.restype = [ctypes.POINTER(config), ctypes.POINTER(buffers)], ctypes.c_int
+            if name != "wdp_norm":
+                query = getattr(lib, name + "_workspace")
+                query.argtypes, query.restype = [ctypes.POINTER(config), size], ctypes.c_int
+        lib.wdp_adamw.argtypes = [ctypes.POINTER(wdp_adamw_config), ctypes.POINTER(wdp_adamw_tensor), ctypes.c_int]
+        lib.wdp_adamw.restype = ctypes.c_int
+        _declared = lib
+    return _declared
+
+
+# ---- the C ABI, one Python function per entry point -------------------------------------------
+def _run(name, *args):
+    rc = getattr(_library(), name)(*args)
+    if rc != WD_OK:
+        raise WdError(rc, name)
+
+
+def _workspace(name, cfg):
+    out = ctypes.c_size_t()
+    _run(name, ctypes.byref(cfg), ctypes.byref(out))
+    return out.value
+
+
+def wdp_norm(cfg, bufs):
+    _run("wdp_norm", ctypes.byref(cfg), ctypes.byref(bufs))
+
+
+def wdp_norm_backward_workspace(cfg):
+    return _workspace("wdp_norm_backward_workspace", cfg)
+
+
+def wdp_norm_backward(cfg, bufs):
+    _run("wdp_norm_backward", ctypes.byref(cfg), ctypes.byref(bufs))
+
+
+def wdp_product_workspace(cfg):
+    return _workspace("wdp_product_workspace", cfg)
+
+
+def wdp_product(cfg, bufs):
+    _run("wdp_product", ctypes.byref(cfg), ctypes.byref(bufs))
+
+
+def wdp_verify_workspace(cfg):
+    return _workspace("wdp_verify_workspace", cfg)
+
+
+def wdp_verify(cfg, bufs):
+    _run("wdp_verify", ctypes.byref(cfg), ctypes.byref(bufs))
+
+
+def wdp_adamw(cfg, tensors, count):
+    _run("wdp_adamw", ctypes.byref(cfg), tensors, count)
+
+
+# ---- tensors ------------------------------------------------------------------------------------
+_FLOATS = _EIGHTS = None
+
+
+def _types():
+    """torch's names of the element types (looked up late: the ABI part of this module works without tensors)."""
+    global _FLOATS, _EIGHTS
+    if _FLOATS is None:
+        import torch
+
+        _FLOATS = {torch.float32: WDP_F32, torch.bfloat16: WDP_BF16, torch.float16: WDP_F16}
+        _EIGHTS = {torch.float8_e4m3fn: WDP_E4M3, torch.float8_e5m2: WDP_E5M2}
+    return _FLOATS, _EIGHTS
+
+
+class _on:
+    """The tensors' device as the current one, and its current stream; raises without a GPU."""
+
+    __slots__ = ("stream", "guard")
+
+    def __init__(self, what, tensor):
+        import torch
+
+        device = tensor.device
+        if device.type != "cuda":
+            raise RuntimeError(f"{what} needs tensors on a GPU: the HIP path has no CPU fallback")
+        self.stream = torch.cuda.current_stream(device).cuda_stream
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.stream
+
+    def __exit__(self, *error):
+        if self.guard is not None:
+            self.guard.__exit__(*error)
+
+
+def _check(what, name, tensor, like, dtypes, shape=None):
+    if tensor.device != like.device:
+        raise ValueError(f"{what}: {name} is on {tensor.device}, not on {like.device}")
+    if tensor.dtype not in dtypes:
+        raise ValueError(f"{what}: {name} has type {tensor.dtype}")
+    if shape is not None and tuple(tensor.shape) != tuple(shape):
+        raise ValueError(f"{what}: {name} has shape {tuple(tensor.shape)}, not {tuple(shape)}")
+
+
+def _rows(what, name, tensor):
+    """(rows, width, stride) of a tensor [..., width] whose rows lie at one stride, elements adjacent."""
+    if tensor.dim() < 1:
+        raise ValueError(f"{what}: {name} has no dimension")
+    width = tensor.shape[-1]
+    if tensor.dim() == 2:
+        rows, stride = tensor.shape[0], tensor.stride(0)
+    elif tensor.is_contiguous():
+        rows, stride = (tensor.numel() // width if width else 0), width
+    else:
+        try:
+            flat = tensor.view(-1, width)
+        except RuntimeError:
+            raise ValueError(f"{what}: the rows of {name} are not at one stride") from None
+        rows, stride = flat.shape[0], flat.stride(0)
+    if rows <= 1 or not width:
+        stride = width
+    if width > 1 and tensor.stride(-1) != 1 or rows > 1 and stride < width:
+        raise ValueError(f"{what}: rows of {name} have to be apart, their elements adjacent")
+    return rows, width, stride
+
+
+NormOut = collections.namedtuple("NormOut", "h y q scale rstd")
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-5, out8=None, y=None, h=None):
+    """RMS norm of ``x`` [..., D], or of ``h = x + residual``; returns NormOut(h, y, q, scale, rstd).
+
+    out8: None gives ``y`` in x's type; ``torch.float8_e4m3fn`` or ``torch.float8_e5m2`` gives ``q`` (rows padded to 16
+    bytes) and ``scale`` [rows, ceil(D / 128)] instead, as ``product8`` takes them, and with ``y=True`` both.
+    h: a tensor to write the sum to (x or residual themselves: in place); a new one otherwise.  Without residual, h is x.
+    rstd: [rows] float32, what ``rms_norm_backward`` needs beside h.  x may be float32, bfloat16 or float16; weight
+    float32 or x's type, None for ones.
+    """
+    import torch
+
+    floats, eights = _types()
+    what = "rms_norm"
+    if x.dtype not in floats:
+        raise ValueError(f"{what}: x has type {x.dtype}")
+    rows, width, x_stride = _rows(what, "x", x)
+    if not width:
+        raise ValueError(f"{what}: x has no elements in a row")
+    if weight is not None:
+        _check(what, "weight", weight, x, (torch.float32, x.dtype), (width,))
+        if not weight.is_contiguous():
+            raise ValueError(f"{what}: weight is not contiguous")
+    if out8 is not None and out8 not in eights:
+        raise ValueError(f"{what}: out8 is {out8}")
+    want_y = out8 is None if y is None else bool(y)
+    if not want_y and out8 is None:
+        raise ValueError(f"{what}: nothing to compute")
+    residual_stride = h_stride = 0
+    if residual is not None:
+        _check(what, "residual", residual, x, (x.dtype,), x.shape)
+        residual_stride = _rows(what, "residual", residual)[2]
+        if h is None:
+            h = torch.empty_like(x, memory_format=torch.contiguous_format)
+        else:
+            _check(what, "h", h, x, (x.dtype,), x.shape)
+        h_stride = _rows(what, "h", h)[2]
+    elif h is not None:
+        raise ValueError(f"{what}: h without a residual")
+    with _on(what, x) as stream:
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_y else None
+        q = scale = None
+        q_stride = -(-width // 16) * 16
+        if out8 is not None:
+            q = torch.empty((rows, q_stride), dtype=out8, device=x.device)
+            # the scales of a block lie side by side: the product reads them row by row of its tiles
+            scale = torch.empty((-(-width // WDP_BLOCK), rows), dtype=torch.float32, device=x.device).t()
+        cfg = wdp_norm_config(ctypes.sizeof(wdp_norm_config), floats[x.dtype], WDP_F32 if weight is None else floats[weight.dtype],
+                              eights[out8] if out8 is not None else 0, rows, width, eps, x_stride, residual_stride, h_stride, width, q_stride,
+                              1, rows, 0, 0, 0, stream)
+        wdp_norm(cfg, wdp_norm_buffers(
+            x.data_ptr(), residual.data_ptr() if residual is not None else None, weight.data_ptr() if weight is not None else None,
+            h.data_ptr() if residual is not None else None, out.data_ptr() if want_y else None, q.data_ptr() if q is not None else None,
+            scale.data_ptr() if q is not None else None, rstd.data_ptr()))
+    return NormOut(x if residual is None else h, out, None if q is None else q[:, :width] if q_stride != width else q, scale, rstd)
+
+
+def rms_norm_backward(dy, h, weight, rstd, dh=None, want_dw=True):
+    """(dx, dw) of ``rms_norm`` from the gradients of y and (``dh``, may be None) of h: dx is the gradient of x and of
+    residual alike, in h's type; dw [D] float32, None with ``want_dw=False``.  weight None: ones."""
+    import torch
+
+    floats, _ = _types()
+    what = "rms_norm_backward"
+    if h.dtype not in floats:
+        raise ValueError(f"{what}: h has type {h.dtype}")
+    rows, width, h_stride = _rows(what, "h", h)
+    if not width:
+        raise ValueError(f"{what}: h has no elements in a row")
+    _check(what, "dy", dy, h, (h.dtype,), h.shape)
+    _check(what, "rstd", rstd, h, (torch.float32,), (rows,))
+    if not rstd.is_contiguous():
+        raise ValueError(f"{what}: rstd is not contiguous")
+    if weight is not None:
+        _check(what, "weight", weight, h, (torch.float32, h.dtype), (width,))
+        if not weight.is_contiguous():
+            raise ValueError(f"{what}: weight is not contiguous")
+    dh_stride = 0
+    if dh is not None:
+        _check(what, "dh", dh, h, (h.dtype,), h.shape)
+        dh_stride = _rows(what, "dh", dh)[2]
+    with _on(what, h) as stream:
+        dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        cfg = wdp_norm_config(ctypes.sizeof(wdp_norm_config), floats[h.dtype], WDP_F32 if weight is None else floats[weight.dtype], 0, rows, width,
+                              0.0, 0, 0, h_stride, 0, 0, 0, 0, _rows(what, "dy", dy)[2], dh_stride, width, stream)
+        dw = space = None
+        if want_dw:
+            dw = torch.empty(width, dtype=torch.float32, device=h.device)
+            space = torch.empty(wdp_norm_backward_workspace(cfg), dtype=torch.uint8, device=h.device)
+        wdp_norm_backward(cfg, wdp_norm_grad_buffers(
+            dy.data_ptr(), dh.data_ptr() if dh is not None else None, h.data_ptr(), weight.data_ptr() if weight is not None else None,
+            rstd.data_ptr(), dx.data_ptr(), dw.data_ptr() if want_dw else None, space.data_ptr() if want_dw else None))
+    return dx, dw
+
+
+def quantise8(w, dtype=None, rows=128):
+    """(codes, scales) of a matrix [n, k] with a scale for each ``rows`` x 128 elements, as ``product8`` takes its second
+    (rows 128 or 1) or first (rows 1) operand.  Plain torch operations, on any device: weights are laid out once."""
+    import torch
+
+    _, eights = _types()
+    dtype = torch.float8_e4m3fn if dtype is None else dtype
+    if dtype not in eights or rows not in (1, 128) or w.dim() != 2:
+        raise ValueError("quantise8: a matrix, an 8-bit type, rows 1 or 128")
+    n, k = w.shape
+    nb, kb = -(-n // rows), -(-k // WDP_BLOCK)
+    cells = torch.zeros((nb * rows, kb * WDP_BLOCK), dtype=torch.float32, device=w.device)
+    cells[:n, :k] = w
+    cells = cells.view(nb, rows, kb, WDP_BLOCK)
+    scale = cells.abs().amax(dim=(1, 3)).clamp_(min=2.0 ** -100) / torch.finfo(dtype).max
+    codes = torch.zeros((n, -(-k // 16) * 16), dtype=dtype, device=w.device)
+    codes[:, :k] = (cells / scale[:, None, :, None]).view(nb * rows, -1)[:n, :k].to(dtype)
+    return codes[:, :k], scale
+
+
+def product8(a, a_scale, b, b_scale, dtype=None, out=None):
+    """``a`` [m, k] times the transpose of ``b`` [n, k], both 8-bit with scales for blocks of 128 along k: [m, n] in
+    ``dtype`` (bfloat16; float32, float16) or into ``out``.  a_scale [m, blocks]; b_scale [ceil(n / 128), blocks], or
+    [n, blocks] for a scale per row; both float32, of any strides.  Rows that start at 16-byte boundaries run faster."""
+    import torch
+
+    floats, eights = _types()
+    what = "product8"
+    if a.dim() != 2 or b.dim() != 2 or a.dtype not in eights:
+        raise ValueError(f"{what}: a is an 8-bit matrix, b another")
+    (m, k, a_stride), (n, kb, b_stride) = _rows(what, "a", a), _rows(what, "b", b)
+    _check(what, "b", b, a, tuple(eights), (n, k))
+    if not k:
+        raise ValueError(f"{what}: a has no elements in a row")
+    blocks, groups = -(-k // WDP_BLOCK), -(-n // WDP_BLOCK)
+    _check(what, "a_scale", a_scale, a, (torch.float32,), (m, blocks))
+    by_row = b_scale.shape[0] == n and n != groups
+    _check(what, "b_scale", b_scale, a, (torch.float32,), (n if by_row else groups, blocks))
+    if out is None:
+        dtype = torch.bfloat16 if dtype is None else dtype
+        if dtype not in floats:
+            raise ValueError(f"{what}: dtype is {dtype}")
+        c_stride = n
+    else:
+        _check(what, "out", out, a, tuple(floats) if dtype is None else (dtype,), (m, n))
+        c_stride = _rows(what, "out", out)[2]
+    with _on(what, a) as stream:
+        if out is None:
+            out = torch.empty((m, n), dtype=dtype, device=a.device)
+        cfg = wdp_product_config(ctypes.sizeof(wdp_product_config), eights[a.dtype], eights[b.dtype], floats[out.dtype], m, n, k,
+                                 1 if by_row else WDP_BLOCK, a_stride, b_stride, c_stride, *a_scale.stride(), *b_scale.stride(), stream)
+        need = wdp_product_workspace(cfg)
+        space = torch.empty(need, dtype=torch.uint8, device=a.device).data_ptr() if need else None
+        wdp_product(cfg, wdp_product_buffers(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), out.data_ptr(), space))
+    return out
+
+
+def verify_drafts(target, draft_probs, drafts, u, lengths=None, tokens=None):
+    """(accepted, tokens): drafted tokens ``drafts`` [B, n] (int32), drawn from ``draft_probs`` [B, n, V], made draws from
+    ``target`` [B, n, V], or [B, n + 1, V] with a row for one more token behind the last draft.  ``u`` [B, n + 1] float32:
+    uniform numbers, n for the drafts and one for the draw; they must not be those that drew the drafts.  lengths [B]
+    int32: how many of a sequence's drafts count.  accepted [B] int32; tokens [B, rows of target] int32: the accepted
+    drafts, the drawn token, -1.  tokens: where to write them (``drafts`` itself where target has n rows)."""
+    import torch
+
+    floats, _ = _types()
+    what = "verify_drafts"
+    if target.dim() != 3 or draft_probs.dim() != 3 or target.dtype not in floats:
+        raise ValueError(f"{what}: target and draft_probs are [B, rows, V]")
+    batch, rows, vocab = target.shape
+    n = draft_probs.shape[1]
+    if not vocab or rows - n not in (0, 1) or rows < 1:
+        raise ValueError(f"{what}: target has {rows} rows for {n} drafts")
+    _check(what, "draft_probs", draft_probs, target, (target.dtype,), (batch, n, vocab))
+    _check(what, "drafts", drafts, target, (torch.int32,), (batch, n))
+    _check(what, "u", u, target, (torch.float32,), (batch, n + 1))
+    for name, t in (("target", target), ("draft_probs", draft_probs)):
+        if vocab > 1 and t.numel() and t.stride(2) != 1:
+            raise ValueError(f"{what}: a row's elements have to be adjacent in {name}")
+    if not (drafts.is_contiguous() and u.is_contiguous()):
+        raise ValueError(f"{what}: drafts and u have to be contiguous")
+    if lengths is not None:
+        _check(what, "lengths", lengths, target, (torch.int32,), (batch,))
+        if not lengths.is_contiguous():
+            raise ValueError(f"{what}: lengths is not contiguous")
+    if tokens is not None:
+        _check(what, "tokens", tokens, target, (torch.int32,), (batch, rows))
+        if not tokens.is_contiguous():
+            raise ValueError(f"{what}: tokens is not contiguous")
+    with _on(what, target) as stream:
+        accepted = torch.empty(batch, dtype=torch.int32, device=target.device)
+        if tokens is None:
+            tokens = torch.empty((batch, rows), dtype=torch.int32, device=target.device)
+        (tb, tr, _), (db, dr, _) = target.stride(), draft_probs.stride()
+        cfg = wdp_verify_config(ctypes.sizeof(wdp_verify_config), floats[target.dtype], batch, n, vocab, rows - n, tb, tr, db, dr, stream)
+        need = wdp_verify_workspace(cfg)
+        space = torch.empty(need, dtype=torch.uint8, device=target.device).data_ptr() if need else None
+        wdp_verify(cfg, wdp_verify_buffers(target.data_ptr(), draft_probs.data_ptr() if n else None, drafts.data_ptr() if n else None,
+                                           lengths.data_ptr() if lengths is not None else None, u.data_ptr(), accepted.data_ptr(),
+                                           tokens.data_ptr(), space))
+    return accepted, tokens
+
+
+class AdamW:
+    """AdamW over the tensors ``params`` with the gradients that stand in ``grads``, in place (lists of equal length; a
+    gradient has its parameter's type or float32).
+
+    The tensors are borrowed: they keep their addresses as long as the optimiser lives, as the environments' buffers do
+    (gradients are accumulated into ``grads`` and cleared with ``zero_()``).  masters: None, or float32 copies that are
+    updated in place of low-precision parameters.  State tensors are allocated (zeros) unless they are given: exp_avg and
+    exp_avg_sq in float32, or with state_bits=8 as float8_e4m3fn, exp_avg_sq holding the root, with float32 scales per 128
+    elements in avg_scale and sq_scale.
+    """
+
+    def __init__(self, params, grads, lr=3e-4, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, seed=0, masters=None,
+                 exp_avg=None, exp_avg_sq=None, avg_scale=None, sq_scale=None):
+        import torch
+
+        floats, _ = _types()
+        what = "AdamW"
+        params, grads = list(params), list(grads)
+        if not params:
+            raise ValueError(f"{what}: no parameters")
+        if state_bits not in (32, 8):
+            raise ValueError(f"{what}: state_bits is {state_bits}")
+        count = len(params)
+        if params[0].device.type != "cuda":
+            raise RuntimeError(f"{what} needs tensors on a GPU: the HIP path has no CPU fallback")
+        state = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+
+        def made(given, dtype, sizes):
+            if given is not None:
+                return list(given)
+            return [torch.zeros(n, dtype=torch.uint8 if dtype == torch.float8_e4m3fn else dtype, device=p.device).view(dtype) for n, p in zip(sizes, params)]
+
+        sizes = [p.numel() for p in params]
+        blocks = [-(-n // WDP_BLOCK) for n in sizes]
+        self.params, self.grads, self.masters = params, grads, None if masters is None else list(masters)
+        self.exp_avg, self.exp_avg_sq = made(exp_avg, state, sizes), made(exp_avg_sq, state, sizes)
+        self.avg_scale, self.sq_scale = (made(s, torch.float32, blocks) if state_bits == 8 else None for s in (avg_scale, sq_scale))
+        self.lr, self.betas, self.eps, self.weight_decay, self.seed, self.state_bits = lr, betas, eps, weight_decay, seed, state_bits
+        self.steps = 0
+        for name, tensors, dtypes, lengths in (("params", params, tuple(floats), sizes), ("grads", grads, tuple(floats), sizes),
+                                               ("masters", self.masters, (torch.float32,), sizes), ("exp_avg", self.exp_avg, (state,), sizes),
+                                               ("exp_avg_sq", self.exp_avg_sq, (state,), sizes), ("avg_scale", self.avg_scale, (torch.float32,), blocks),
+                                               ("sq_scale", self.sq_scale, (torch.float32,), blocks)):
+            if tensors is None:
+                continue
+            if len(tensors) != count:
+                raise ValueError(f"{what}: {len(tensors)} {name} for {count} parameters")
+            for t, n in zip(tensors, lengths):
+                _check(what, name, t, params[0], dtypes)
+                if t.numel() != n or not t.is_contiguous():
+                    raise ValueError(f"{what}: {name} have to be contiguous and of their parameter's size")
+        for p, g in zip(params, grads):
+            if g.dtype not in (torch.float32, p.dtype):
+                raise ValueError(f"{what}: a gradient has type {g.dtype}, its parameter {p.dtype}")
+
+        def ptr(tensors, i):
+            return tensors[i].data_ptr() if tensors is not None else None
+
+        self._table = (wdp_adamw_tensor * count)(*[
+            wdp_adamw_tensor(params[i].data_ptr(), grads[i].data_ptr(), ptr(self.masters, i), ptr(self.exp_avg, i), ptr(self.exp_avg_sq, i),
+                             ptr(self.avg_scale, i), ptr(self.sq_scale, i), sizes[i], floats[params[i].dtype], floats[grads[i].dtype])
+            for i in range(count)])
+
+    def step(self, step=None, step_device=None, grad_scale=None):
+        """One update.  step: its number (one more than the last by default).  step_device: an int64 device tensor that
+        holds the number when the kernel runs, for steps captured into a HIP graph.  grad_scale: a float32 device tensor
+        that the gradients are multiplied by (a clipping factor)."""
+        import torch
+
+        what = "AdamW.step"
+        first = self.params[0]
+        if step_device is not None:
+            _check(what, "step_device", step_device, first, (torch.int64,))
+        if grad_scale is not None:
+            _check(what, "grad_scale", grad_scale, first, (torch.float32,))
+        for t in (step_device, grad_scale):
+            if t is not None and t.numel() != 1:
+                raise ValueError(f"{what}: one number on the device, not {t.numel()}")
+        number = self.steps + 1 if step is None else int(step)
+        with _on(what, first) as stream:
+            wdp_adamw(wdp_adamw_config(ctypes.sizeof(wdp_adamw_config), self.state_bits, self.lr, self.betas[0], self.betas[1], self.eps,
+                                       self.weight_decay, number, step_device.data_ptr() if step_device is not None else None,
+                                       grad_scale.data_ptr() if grad_scale is not None else None, self.seed, stream),
+                      self._table, len(self.params))
+        self.steps = number

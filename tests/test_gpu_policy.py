@@ -1,0 +1,647 @@
+"""The policy's operators on the GPU against float64 references: values, gradients, edges, streams, graphs, the run together."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2108_13976_amd as wd
+from paper_2108_13976_amd import policy
+
+import policy_refs as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+E4M3, E5M2 = torch.float8_e4m3fn, torch.float8_e5m2
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+EPS24 = 2.0 ** -24
+
+
+def generator(*key):
+    return torch.Generator().manual_seed(sum(k * 7919 ** i for i, k in enumerate(key)) % (1 << 31))
+
+
+def normal(gen, *shape, dtype=F32, scale=1.0):
+    return (torch.randn(shape, generator=gen) * scale).to(dtype).to(DEV)
+
+
+# ---- norm ---------------------------------------------------------------------------------------
+def check_norm(x, weight, residual, eps, out, out8):
+    """Float32 errors: a sum of `width` squares in chains of at most width / 4 adds and 16 levels, halved by the root; four
+    more operations on the way to y (product with rstd, with the weight, the root, the quotient)."""
+    width = x.shape[1]
+    h, y, rstd = ref.norm(x, weight, residual, eps)
+    rel = ((width / 4 + 16) / 2 + 6) * EPS24
+    assert torch.equal(out.h.cpu(), h), "h"
+    assert ((ref.f64(out.rstd) - rstd).abs() <= rel * rstd).all(), "rstd"
+    if out.y is not None:
+        assert ((ref.f64(out.y) - y).abs() <= rel * y.abs() + ref.rounding(y * (1 + rel), x.dtype) + 1e-38).all(), "y"
+    if out8 is None:
+        assert out.q is None and out.scale is None
+        return
+    scale = torch.stack([b.abs().amax(1) for b in ref.blocks_of(y)], 1).clamp(min=ref.TINY) / ref.LARGEST[out8]
+    assert ((ref.f64(out.scale) - scale).abs() <= (rel + 3 * EPS24) * scale).all(), "scale"
+    z = y / scale.repeat_interleave(128, 1)[:, :width]
+    off = (out.q.cpu().float().double() - z).abs()
+    assert (off <= ref.rounding(z, out8) * (1 + 1e-6) + 2 * (rel + 4 * EPS24) * z.abs()).all(), "q"
+
+
+WIDTHS = [1, 5, 8, 21, 32, 33, 64, 65, 127, 128, 129, 200, 256, 257, 511, 512, 777, 1000, 1024, 1025, 2048, 2049, 2999, 4096, 5001, 8192, 8193, 16384, 16385, 32768]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("width", WIDTHS)
+def test_norm_against_float64(width, dtype):
+    gen = generator(width, 3)
+    for rows, with_residual, out8, weight_dtype in ((1, True, E4M3, F32), (3, False, None, dtype), (71, True, E5M2, dtype)):
+        x, r = normal(gen, rows, width, dtype=dtype), normal(gen, rows, width, dtype=dtype, scale=2.0) if with_residual else None
+        w = (1 + 0.2 * torch.randn(width, generator=gen)).to(weight_dtype).to(DEV)
+        out = wd.rms_norm(x, w, residual=r, eps=1e-5, out8=out8, y=True)
+        check_norm(x, w, r, 1e-5, out, out8)
+
+
+@pytest.mark.parametrize("rows,width", [(20011, 21), (9001, 256), (2500, 999), (700, 3000)])
+def test_norm_of_more_rows_than_a_launch_holds_at_once(rows, width):
+    gen = generator(rows, width)
+    x, r = normal(gen, rows, width, dtype=BF16), normal(gen, rows, width, dtype=BF16)
+    check_norm(x, None, r, 1e-6, wd.rms_norm(x, None, residual=r, eps=1e-6, out8=E4M3), E4M3)
+
+
+def test_norm_of_rows_that_are_zero_tiny_large_or_not_finite():
+    gen = generator(1, 2)
+    for width in (40, 300, 2100):
+        x = normal(gen, 8, width)
+        x[0] = 0
+        x[1] *= 1e-30   # below the least maximum of a block once weighted, with eps 0 brought back to one
+        x[2] *= 1e15
+        x[3, 7] = float("nan")
+        x[4, 7] = float("inf")
+        x[5, :30] = 0
+        w = torch.ones(width, device=DEV)
+        out = wd.rms_norm(x, w, eps=1e-5, out8=E4M3, y=True)
+        fine = [0, 1, 2, 5, 6, 7]
+        pick = wd.NormOut(out.h[fine], out.y[fine], out.q[fine], out.scale[fine], out.rstd[fine])
+        check_norm(x[fine], w, None, 1e-5, pick, E4M3)
+        assert out.q[0].float().abs().max() == 0 and out.scale[0].isfinite().all()
+        assert out.y[3].isnan().all() and out.q[3].float().isnan().all() and out.rstd[3].isnan()
+        bad = torch.zeros(width, dtype=torch.bool)
+        bad[7] = True
+        assert torch.equal(out.y[4].isnan().cpu(), bad) and torch.equal(out.q[4].float().isnan().cpu(), bad)
+        assert (out.y[4][~bad.to(DEV)] == 0).all() and out.rstd[4] == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width,pitch,offset", [(21, 24, 0), (21, 23, 1), (256, 264, 0), (255, 261, 3), (1500, 1503, 1), (5000, 5003, 1)])
+def test_norm_of_strided_rows_in_place_and_what_lies_beside_them(width, pitch, offset, dtype):
+    gen = generator(width, pitch, offset)
+    rows = 37
+    store_x, store_r = normal(gen, rows + 2, pitch + offset, dtype=dtype), normal(gen, rows + 2, pitch + offset, dtype=dtype)
+    x, r = store_x[1:-1, offset:offset + width], store_r[1:-1, offset:offset + width]
+    before, kept, x0, r0 = store_r.clone(), store_x.clone(), x.clone(), r.clone()
+    out = wd.rms_norm(x, None, residual=r, h=r, out8=E4M3, y=True)
+    check_norm(x0, None, r0, 1e-5, out, E4M3)
+    assert out.h.data_ptr() == r.data_ptr() and torch.equal(store_x, kept)
+    before[1:-1, offset:offset + width] = r
+    assert torch.equal(store_r, before)
+
+
+def raw_norm(rows, width, dtype_code, **over):
+    cfg = policy.wdp_norm_config(ctypes.sizeof(policy.wdp_norm_config), dtype_code, policy.WDP_F32, policy.WDP_E4M3, rows, width, 1e-5,
+                                 width, width, width, width, width, -(-width // 128), 1, width, width, width, torch.cuda.current_stream().cuda_stream)
+    for n, v in over.items():
+        setattr(cfg, n, v)
+    return cfg
+
+
+def test_norm_writes_nothing_beyond_its_outputs():
+    rows, width = 13, 77
+    gen = generator(5)
+    x = normal(gen, rows, width, dtype=BF16)
+    guard = 64
+    q = torch.full((rows * 96 + guard,), 0x55, dtype=torch.uint8, device=DEV)
+    scale, rstd = torch.full((rows * 3 + guard,), 7.0, device=DEV), torch.full((rows + guard,), 7.0, device=DEV)
+    y = torch.full((rows * 80 + guard,), 7.0, dtype=BF16, device=DEV)
+    cfg = raw_norm(rows, width, policy.WDP_BF16, q_stride=96, scale_row_stride=3, y_stride=80)
+    wd.wdp_norm(cfg, policy.wdp_norm_buffers(x.data_ptr(), None, None, None, y.data_ptr(), q.data_ptr(), scale.data_ptr(), rstd.data_ptr()))
+    torch.cuda.synchronize()
+    assert (q[:rows * 96].view(rows, 96)[:, width:] == 0x55).all() and (q[rows * 96:] == 0x55).all()
+    assert (scale[:rows * 3].view(rows, 3)[:, 1:] == 7).all() and (scale[rows * 3:] == 7).all() and (rstd[rows:] == 7).all()
+    assert (y[:rows * 80].view(rows, 80)[:, width:] == 7).all() and (y[rows * 80:] == 7).all()
+    check_norm(x, None, None, 1e-5, wd.NormOut(x, y[:rows * 80].view(rows, 80)[:, :width], q[:rows * 96].view(rows, 96)[:, :width].view(E4M3),
+                                               scale[:rows * 3].view(rows, 3)[:, :1], rstd[:rows]), E4M3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,width", [(1, 1), (2, 5), (50, 21), (300, 64), (1000, 100), (77, 256), (4500, 256), (33, 333), (2600, 999), (40, 1024), (9, 2048),
+                                        (600, 2999), (3, 8192), (700, 5000), (5, 16385), (2, 32768)])
+def test_norm_gradients_against_float64(rows, width, dtype):
+    """dx: the mean of width products in chains of at most width / 4 adds and 16 levels, a handful of operations more; dw: rows
+    products (two operations each), chains of at most rows adds."""
+    gen = generator(rows, width)
+    h, dy, dh = (normal(gen, rows, width, dtype=dtype, scale=s) for s in (2.0, 1.0, 0.5))
+    w = 1 + 0.2 * normal(gen, width)
+    rstd = torch.rsqrt(h.float().square().mean(1) + 1e-5)
+    for extra, weight in ((dh, w), (None, w.to(dtype)), (None, None)):
+        dx, dw = wd.rms_norm_backward(dy, h, weight, rstd, dh=extra)
+        want_dx, want_dw, size_dx, size_dw = ref.norm_backward(dy, h, weight, rstd, extra)
+        assert ((ref.f64(dx) - want_dx).abs() <= (width / 4 + 24) * EPS24 * size_dx + ref.rounding(want_dx, dtype) * 1.01 + 1e-30).all(), "dx"
+        assert ((ref.f64(dw) - want_dw).abs() <= (rows + 40) * EPS24 * size_dw + 1e-30).all(), "dw"
+        again_dx, again_dw = wd.rms_norm_backward(dy, h, weight, rstd, dh=extra)
+        assert torch.equal(dx, again_dx) and torch.equal(dw, again_dw), "the same in every run"
+        only, none = wd.rms_norm_backward(dy, h, weight, rstd, dh=extra, want_dw=False)
+        assert none is None and torch.equal(only, dx)
+
+
+def test_norm_gradients_against_differences():
+    """The loss sum(c * y + d * h) along random directions: central differences of the forward kernel's own float32 outputs.
+    Step 2^-6: the third derivative's part is about 2^-12 / 6 of the slope's size, the outputs' rounding 2^-24 / 2^-6 of the
+    terms' sizes at each of them (their root sum of squares is far below their sum): 2e-3 of the slope's size covers both."""
+    gen = generator(8)
+    rows, width, step = 40, 200, 2.0 ** -6
+    x, r, c, d = (normal(gen, rows, width) for _ in range(4))
+    w = 1 + 0.2 * normal(gen, width)
+
+    def loss(x, r, w):
+        out = wd.rms_norm(x, w, residual=r, eps=1e-5)
+        return float((ref.f64(out.y) * ref.f64(c) + ref.f64(out.h) * ref.f64(d)).sum())
+
+    out = wd.rms_norm(x, w, residual=r, eps=1e-5)
+    dx, dw = wd.rms_norm_backward(c, out.h, w, out.rstd, dh=d)
+    for which in range(3):
+        to = normal(gen, width) if which == 2 else normal(gen, rows, width)
+        args = [x, r, w]
+        up, down = list(args), list(args)
+        up[which], down[which] = args[which] + step * to, args[which] - step * to
+        slope = (loss(*up) - loss(*down)) / (2 * step)
+        grad = dw if which == 2 else dx
+        size = float((ref.f64(grad) * ref.f64(to)).square().sum().sqrt())
+        assert abs(slope - float((ref.f64(grad) * ref.f64(to)).sum())) <= 2e-3 * max(size, 1.0) * 4, which
+
+
+def test_norm_gradients_in_place_and_strided():
+    gen = generator(9)
+    rows, width = 50, 130
+    store = normal(gen, rows, 160, dtype=BF16)
+    h, dy = store[:, 3:133], normal(gen, rows, width, dtype=BF16)
+    rstd = torch.rsqrt(h.float().square().mean(1) + 1e-5)
+    want, dw = wd.rms_norm_backward(dy, h.contiguous(), None, rstd)
+    got, dw2 = wd.rms_norm_backward(dy, h, None, rstd)
+    assert torch.equal(want, got) and torch.equal(dw, dw2)
+    cfg = raw_norm(rows, width, policy.WDP_BF16, h_stride=160)
+    wd.wdp_norm_backward(cfg, policy.wdp_norm_grad_buffers(dy.data_ptr(), None, h.data_ptr(), None, rstd.data_ptr(), dy.data_ptr(), None, None))
+    assert torch.equal(dy, want)
+
+
+# ---- product --------------------------------------------------------------------------------------
+def operands(gen, m, n, k, a_type=E4M3, b_type=E4M3, by_row=False):
+    a, a_scale = wd.quantise8(normal(gen, m, k) * torch.exp(normal(gen, m, 1)), a_type, rows=1)
+    b, b_scale = wd.quantise8(normal(gen, n, k), b_type, rows=1 if by_row else 128)
+    return a, a_scale, b, b_scale
+
+
+def check_product(a, a_scale, b, b_scale, by_row, c):
+    """A block's 128 products are exact in float32 (8 significant bits); 127 adds in whatever order, each off by a step at
+    most (an adder that truncates), then two operations a block with the scales."""
+    want, size = ref.product(a, a_scale, b, b_scale, by_row)
+    blocks = a_scale.shape[1]
+    assert ((ref.f64(c) - want).abs() <= (2 * 127 + 2 * blocks + 4) * EPS24 * size + ref.rounding(want, c.dtype) * 1.01 + 1e-38).all()
+
+
+SIZES = [(1, 1, 1), (1, 5, 21), (2, 3, 127), (5, 128, 128), (16, 17, 129), (17, 16, 255), (50, 256, 256), (33, 129, 1000), (64, 64, 64), (100, 333, 384),
+         (129, 127, 130), (200, 40, 2048), (257, 300, 515), (1000, 5, 64), (1, 4096, 512), (7, 1000, 4096), (16, 130, 16384), (300, 513, 1024), (512, 512, 640)]
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("a_type,b_type,by_row,dtype", [(E4M3, E4M3, False, BF16), (E5M2, E4M3, True, F32), (E4M3, E5M2, False, F16), (E5M2, E5M2, True, BF16)])
+def test_product_against_float64(m, n, k, a_type, b_type, by_row, dtype):
+    gen = generator(m, n, k)
+    a, a_scale, b, b_scale = operands(gen, m, n, k, a_type, b_type, by_row)
+    if dtype == F16:  # within the type's range
+        a_scale = a_scale * 0.01
+    check_product(a, a_scale, b, b_scale, by_row and n != -(-n // 128), wd.product8(a, a_scale, b, b_scale, dtype=dtype))
+
+
+@pytest.mark.parametrize("m,n,k,by_row", [(2048, 1024, 512, False), (2100, 1000, 700, False), (4096, 256, 256, False), (5003, 256, 256, False), (3000, 200, 200, True), (1500, 1537, 1100, True)])
+def test_product_of_many_rows(m, n, k, by_row):
+    gen = generator(m, n, k)
+    args = operands(gen, m, n, k, by_row=by_row)
+    for dtype in (BF16, F32):
+        check_product(*args, by_row, wd.product8(*args, dtype=dtype))
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 40, 100), (40, 200, 300), (300, 260, 520), (2500, 256, 256)])
+@pytest.mark.parametrize("pitch_a,pitch_b,pitch_c", [(0, 0, 0), (16, 32, 8), (3, 5, 1), (1, 16, 7)])
+def test_product_of_strided_rows_with_anything_behind_them(m, n, k, pitch_a, pitch_b, pitch_c):
+    """NaN codes behind the rows and a guard around c."""
+    gen = generator(m, n, k, pitch_a)
+    a, a_scale, b, b_scale = operands(gen, m, n, k)
+
+    def wide(t, pitch):
+        store = torch.full((t.shape[0] + 1, k + pitch), 0x7F, dtype=torch.uint8, device=DEV)
+        store[:-1, :k] = t.contiguous().view(torch.uint8)
+        return store.view(t.dtype)[:-1, :k]
+
+    c = torch.full((m + 1, n + pitch_c + 1), 3.0, device=DEV)
+    by_blocks = torch.empty((a_scale.shape[1], m), device=DEV).t()
+    by_blocks.copy_(a_scale)
+    wd.product8(wide(a, pitch_a), by_blocks, wide(b, pitch_b), b_scale, out=c[:m, :n])
+    check_product(a, a_scale, b, b_scale, False, c[:m, :n])
+    assert (c[m:] == 3).all() and (c[:, n:] == 3).all()
+
+
+def test_product_of_codes_that_are_not_finite():
+    gen = generator(77)
+    for m, n, k in ((4, 20, 300), (200, 300, 300), (2200, 256, 256)):
+        a, a_scale, b, b_scale = operands(gen, m, n, k)
+        fine = wd.product8(a, a_scale, b, b_scale, dtype=F32)
+        a.view(torch.uint8)[m // 2, 200] = 0x7F
+        b.view(torch.uint8)[n // 3, 250] = 0xFF
+        a_scale[1, 0] = float("inf")
+        got = wd.product8(a, a_scale, b, b_scale, dtype=F32)
+        assert got[m // 2].isnan().all() and got[:, n // 3].isnan().all() and not got[1].isfinite().any()
+        rows, cols = torch.ones(m, dtype=torch.bool, device=DEV), torch.ones(n, dtype=torch.bool, device=DEV)
+        rows[[1, m // 2]], cols[n // 3] = False, False
+        assert torch.equal(got[rows][:, cols], fine[rows][:, cols])
+
+
+def test_product_of_infinite_e5m2_codes():
+    a, a_scale = torch.ones((3, 130), device=DEV).to(E5M2), torch.ones((3, 2), device=DEV)
+    b, b_scale = torch.ones((5, 130), device=DEV).to(E4M3), torch.ones((1, 2), device=DEV)
+    a[1, 129] = float("inf")
+    c = wd.product8(a, a_scale, b, b_scale, dtype=F32)
+    assert (c[1] == float("inf")).all() and (c[[0, 2]] == 130).all()
+
+
+def test_product_gives_the_same_in_every_run():
+    gen = generator(4)
+    for m, n, k in ((8, 512, 8192), (1000, 300, 700), (4096, 512, 512)):
+        args = operands(gen, m, n, k)
+        first = wd.product8(*args)
+        for _ in range(3):
+            assert torch.equal(first, wd.product8(*args))
+
+
+# ---- verification ------------------------------------------------------------------------------------
+def drafts_of(gen, batch, n, vocab, bonus, dtype=F32, near=0.7):
+    logits = 2 * torch.randn((batch, n + bonus, vocab), generator=gen)
+    p = torch.softmax(logits, -1).to(dtype)
+    q = torch.softmax(logits[:, :n] + near * torch.randn((batch, n, vocab), generator=gen), -1).to(dtype)
+    x = torch.multinomial(q.float().view(-1, vocab) + 1e-30, 1, generator=gen).view(batch, n).int() if n else torch.zeros((batch, 0), dtype=torch.int32)
+    u = torch.randint(0, 1 << 24, (batch, n + 1), generator=gen).float() / (1 << 24)
+    return [t.to(DEV) for t in (p, q, x, u)]
+
+
+def check_verify(p, q, x, u, lengths=None, **how):
+    accepted, tokens = wd.verify_drafts(p, q, x, u, lengths=lengths, **how)
+    want_accepted, want_tokens = ref.verify(p, q, x, u, lengths)
+    assert np.array_equal(accepted.cpu().numpy(), want_accepted)
+    assert np.array_equal(tokens.cpu().numpy(), want_tokens)
+    return accepted, tokens
+
+
+VERIFY = [(1, 1, 1), (700, 1, 5), (257, 3, 5), (64, 8, 2), (33, 2, 16), (40, 4, 17), (21, 1, 100), (9, 3, 1000), (5, 64, 64), (12, 2, 1023), (12, 2, 1024), (7, 3, 1025),
+          (6, 4, 4095), (6, 4, 4096), (5, 3, 4097), (4, 2, 8192), (3, 5, 9999), (2, 1, 50000), (1, 2, 131073)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("batch,n,vocab", VERIFY)
+def test_verify_against_the_definition(batch, n, vocab, dtype):
+    gen = generator(batch, n, vocab)
+    for bonus in (0, 1):
+        args = drafts_of(gen, batch, n, vocab, bonus, dtype)
+        check_verify(*args)
+        lengths = torch.randint(-1, n + 2, (batch,), generator=gen, dtype=torch.int32).to(DEV)
+        check_verify(*args, lengths=lengths)
+
+
+@pytest.mark.parametrize("vocab", [5, 16, 17, 300, 3000, 10000])
+def test_verify_edges(vocab):
+    """Everything accepted, everything refused, no probability left, tokens out of range, numbers at the ends."""
+    gen = generator(vocab)
+    batch, n = 12, 3
+    p, q, x, u = drafts_of(gen, batch, n, vocab, 1)
+    u[:, :] = 0.0
+    check_verify(p, q, x, u)                       # accepted as long as p(x) > 0; the draw is the first with r > 0
+    u[:, :] = 1.0 - 2.0 ** -24
+    check_verify(p, q, x, u)
+    check_verify(q[:, [0, 1, 2, 2]].clone(), q, x, u)  # p = q: u < 1 accepts everything
+    p2 = p.clone()
+    p2[:, 0] = 0.5 * q[:, 0]                       # refused at 0 with nothing left of p - q: a draw from p
+    check_verify(p2, q, x, u)
+    p2[:, 0] = 0.0                                 # and with p empty: the last token
+    _, tokens = check_verify(p2, q, x, u)
+    assert (tokens[:, 0] == vocab - 1).all()
+    p3 = torch.zeros_like(p)
+    p3[:, :, vocab // 2] = 1.0                     # all on one token
+    _, tokens = check_verify(p3, q, x, u)
+    x2 = x.clone()
+    x2[0], x2[1], x2[2, 1], x2[3] = -1, vocab, 1 << 30, -(1 << 31)
+    u = torch.rand((batch, n + 1), generator=gen).to(DEV)
+    accepted, _ = check_verify(p, q, x2, u)
+    assert accepted[0] == 0 and accepted[1] == 0 and accepted[2] <= 1 and accepted[3] == 0
+    check_verify(p * 3.7, q * 0.2, x, u)           # not normalised
+    p4, q4 = p.clone(), q.clone()
+    p4[:, :, 1], q4[:, :, 2], p4[:, 1, 3] = float("nan"), float("nan"), -1.0
+    check_verify(p4, q4, x, u)
+    u[::2, 1] = float("nan")
+    u[1::2, n] = float("nan")
+    check_verify(p, q, x, u)
+
+
+@pytest.mark.parametrize("vocab", [5, 200, 2000, 9000])
+def test_verify_with_infinite_probabilities(vocab):
+    gen = generator(vocab, 1)
+    p, q, x, u = drafts_of(gen, 8, 2, vocab, 1)
+    p[::2, :, vocab // 3] = float("inf")
+    check_verify(p, q, x, u)
+
+
+def test_verify_without_drafts_is_a_draw():
+    gen = generator(3)
+    for vocab in (5, 500, 7000):
+        p, q, x, u = drafts_of(gen, 30, 0, vocab, 1)
+        accepted, tokens = check_verify(p, q, x, u)
+        assert (accepted == 0).all() and (tokens >= 0).all()
+
+
+def test_verify_in_place_strided_and_many_sequences():
+    gen = generator(6)
+    p, q, x, u = drafts_of(gen, 70001, 1, 5, 0)
+    drafted = x.clone()
+    accepted, tokens = wd.verify_drafts(p, q, x, u, tokens=x)
+    want_accepted, want_tokens = ref.verify(p, q, drafted, u)
+    assert tokens.data_ptr() == x.data_ptr() and np.array_equal(x.cpu().numpy(), want_tokens) and np.array_equal(accepted.cpu().numpy(), want_accepted)
+    for vocab in (5, 600, 5000):
+        p, q, x, u = drafts_of(gen, 9, 3, vocab, 1)
+        wide_p, wide_q = torch.full((9, 5, vocab + 3), float("nan"), device=DEV), torch.full((9, 4, vocab + 1), float("nan"), device=DEV)
+        wide_p[:, :4, 1:vocab + 1], wide_q[:, :3, :vocab] = p, q
+        check_verify(wide_p[:, :4, 1:vocab + 1], wide_q[:, :3, :vocab], x, u)
+        first = p[:1].expand(9, -1, -1)  # one target for all sequences: a batch stride of zero
+        check_verify(first, q, x, u)
+
+
+def test_verified_drafts_are_draws_from_the_target():
+    """Chi-square over 200 000 sequences, whatever q is: 4 degrees of freedom, 33.4 is passed with probability 1e-6."""
+    gen = generator(12)
+    batch = 200000
+    p = torch.tensor([0.05, 0.4, 0.25, 0.2, 0.1])
+    for q in (torch.tensor([0.3, 0.1, 0.2, 0.2, 0.2]), torch.tensor([0.96, 0.01, 0.01, 0.01, 0.01]), p.clone()):
+        x = torch.multinomial(q, batch, replacement=True, generator=gen).int().view(-1, 1)
+        u = torch.rand((batch, 2), generator=gen)
+        _, tokens = wd.verify_drafts(p.to(DEV).expand(batch, 1, 5), q.to(DEV).expand(batch, 1, 5), x.to(DEV), u.to(DEV))
+        counts = torch.bincount(tokens[:, 0].long().cpu(), minlength=5).double()
+        assert float(((counts - batch * p.double()) ** 2 / (batch * p.double())).sum()) < 33.4
+
+
+# ---- AdamW ------------------------------------------------------------------------------------------
+HYPER = dict(lr=3e-4, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01)
+NUMELS = [1, 5, 7, 8, 100, 127, 128, 129, 1000, 2048, 2049, 5000, 0, 64]
+
+
+def tensors_of(gen, sizes, dtype, grad_dtype=None, scale=0.05):
+    params = [normal(gen, n, dtype=dtype, scale=scale) for n in sizes]
+    grads = [normal(gen, n, dtype=grad_dtype or dtype, scale=0.01) for n in sizes]
+    return params, grads
+
+
+def near(got, want, steps, scale=None):
+    """Within `steps` float32 roundings of the terms' size."""
+    return ((ref.f64(got) - want).abs() <= steps * EPS24 * (want.abs() if scale is None else scale) + 1e-36).all()
+
+
+@pytest.mark.parametrize("dtype,grad_dtype,with_master", [(F32, F32, False), (BF16, BF16, True), (BF16, F32, True), (F16, F16, False), (BF16, BF16, False), (F16, F32, True)])
+def test_adamw_against_float64_over_three_steps(dtype, grad_dtype, with_master):
+    """From the state that stands before each step: m, v are three operations each (of terms no larger than their sizes added),
+    p eight more on the update, whose size is lr times a quotient."""
+    gen = generator(21)
+    params, grads = tensors_of(gen, NUMELS, dtype, grad_dtype)
+    masters = [p.float() for p in params] if with_master else None
+    opt = wd.AdamW(params, grads, masters=masters, **HYPER)
+    for step in (1, 2, 3):
+        for g in grads:
+            g.copy_(torch.randn(g.shape, generator=gen) * 0.01)
+        before = [(ref.f64(masters[i] if with_master else params[i]), ref.f64(grads[i]), ref.f64(opt.exp_avg[i]), ref.f64(opt.exp_avg_sq[i])) for i in range(len(params))]
+        opt.step()
+        for i, (p, g, m, v) in enumerate(before):
+            want_p, want_m, want_v = ref.adamw(p, g, m, v, step, **{"lr": HYPER["lr"], "betas": HYPER["betas"], "eps": HYPER["eps"], "decay": HYPER["weight_decay"]})
+            assert near(opt.exp_avg[i], want_m, 4, 0.9 * m.abs() + 0.1 * g.abs()), ("m", step, i)
+            assert near(opt.exp_avg_sq[i], want_v, 6), ("v", step, i)
+            # the quotient's relative error: m's absolute one over its size included
+            moved = (want_p - p).abs() + HYPER["lr"] * 2 * (0.9 * m.abs() + 0.1 * g.abs()) / (1 - 0.9 ** step) / (torch.sqrt(want_v / (1 - 0.999 ** step)) + 1e-8)
+            allowed = 4 * EPS24 * p.abs() + 16 * EPS24 * moved + 1e-36
+            if with_master:
+                assert ((ref.f64(masters[i]) - want_p).abs() <= allowed).all(), ("master", step, i)
+                assert torch.equal(params[i], masters[i].to(dtype))
+            else:
+                assert ((ref.f64(params[i]) - want_p).abs() <= allowed + (ref.rounding(want_p, dtype) * 1.01 if dtype != F32 else 0)).all(), ("p", step, i)
+    assert opt.steps == 3
+
+
+def test_adamw_of_more_tensors_than_a_launch_takes_and_of_mixed_types():
+    gen = generator(22)
+    sizes = [(37 * i) % 301 for i in range(130)]
+    params = [normal(gen, n, dtype=(F32, BF16, BF16, F16)[i // 20 % 4], scale=0.05) for i, n in enumerate(sizes)]
+    grads = [normal(gen, n, dtype=p.dtype if i % 7 else F32, scale=0.01) for i, (n, p) in enumerate(zip(sizes, params))]
+    masters = [p.float() for p in params]
+    for bits in (32, 8):
+        a = wd.AdamW([p.clone() for p in params], grads, masters=[m.clone() for m in masters], state_bits=bits, seed=5, **HYPER)
+        a.step()
+        for i in range(len(params)):
+            want, m, v = ref.adamw(ref.f64(masters[i]), ref.f64(grads[i]), 0.0, 0.0, 1, HYPER["lr"], HYPER["betas"], HYPER["eps"], HYPER["weight_decay"])
+            assert ((ref.f64(a.masters[i]) - want).abs() <= 4 * EPS24 * ref.f64(masters[i]).abs() + 20 * EPS24 * HYPER["lr"]).all(), i
+
+
+def test_adamw_leaves_what_lies_between_the_tensors():
+    gen = generator(23)
+    for bits in (32, 8):
+        store = {n: torch.full((4000,), 0.25, device=DEV) for n in ("p", "g", "m", "v")}
+        spans = [(1, 130), (131, 7), (140, 2050), (2300, 1000)]
+        views = {n: [t[a:a + k] for a, k in spans] for n, t in store.items()}
+        if bits == 8:
+            eight = {n: torch.full((4000,), 0x38, dtype=torch.uint8, device=DEV).view(E4M3) for n in ("m", "v")}
+            views.update({n: [t[a:a + k] for a, k in spans] for n, t in eight.items()})
+            scales = {n: torch.full((64,), 0.25, device=DEV) for n in ("a", "s")}
+            views.update({n: [t[i * 18:i * 18 + -(-k // 128)] for i, (_, k) in enumerate(spans)] for n, t in scales.items()})
+        opt = wd.AdamW(views["p"], views["g"], state_bits=bits, exp_avg=views["m"], exp_avg_sq=views["v"],
+                       avg_scale=views["a"] if bits == 8 else None, sq_scale=views["s"] if bits == 8 else None, **HYPER)
+        opt.step()
+        inside = torch.zeros(4000, dtype=torch.bool, device=DEV)
+        for a, k in spans:
+            inside[a:a + k] = True
+        assert (store["p"][~inside] == 0.25).all() and (store["p"][inside] != 0.25).all() and (store["g"] == 0.25).all()
+        if bits == 32:
+            assert (store["v"][~inside] == 0.25).all() and (store["v"][inside] != 0.25).all()
+        else:
+            assert all((t.view(torch.uint8)[~inside] == 0x38).all() for t in eight.values())
+            for t in scales.values():
+                assert sum(int(x) for x in t != 0.25) == sum(-(-k // 128) for _, k in spans)
+
+
+def test_adamw_8_bit_states_are_the_documented_roundings():
+    """Each code is where the definition puts it, from the state before the step: units of the code's step plus the random
+    fraction, downwards; one apart where that comes within 1e-4 of a whole number (float32: the quotient is off by a few 2^-24
+    of at most 16 units, which is below 1e-5)."""
+    gen = generator(24)
+    sizes = [1000, 3, 128, 517]
+    params, grads = tensors_of(gen, sizes, F32)
+    opt = wd.AdamW(params, grads, state_bits=8, seed=(7 << 32) + 99, **HYPER)
+    for step in (1, 2, 3, (3 << 32) + 5):
+        for g in grads:
+            g.copy_(torch.randn(g.shape, generator=gen) * torch.exp(3 * torch.randn(g.shape, generator=gen)) * 0.01)
+        before = [[ref.f64(t[i].float()) for t in (opt.params, opt.grads, opt.exp_avg, opt.exp_avg_sq)] +
+                  [ref.f64(s[i]).repeat_interleave(128)[:n] for s in (opt.avg_scale, opt.sq_scale)] for i, n in enumerate(sizes)]
+        opt.step(step=step)
+        blocks = 0
+        for i, n in enumerate(sizes):
+            p, g, m, s, ms, ss = before[i]
+            want_p, m, v = ref.adamw(p, g, m * ms, (s * ss) ** 2, step, HYPER["lr"], HYPER["betas"], HYPER["eps"], HYPER["weight_decay"])
+            assert ((ref.f64(opt.params[i]) - want_p).abs() <= 4 * EPS24 * p.abs() + 30 * EPS24 * (want_p - p).abs() + 1e-12).all()
+            at = np.arange(n, dtype=np.uint64) + np.uint64(128 * blocks)
+            words = ref.philox_words((7 << 32) + 99, at // np.uint64(4), step)[np.arange(n), (at % np.uint64(4)).astype(int)]
+            blocks += -(-n // 128)
+            for value, codes, scales, bits in ((m, opt.exp_avg[i], opt.avg_scale[i], words & np.uint64(0xFFFF)), (v.sqrt(), opt.exp_avg_sq[i], opt.sq_scale[i], words >> np.uint64(16))):
+                want_scale = torch.stack([b.abs().max() for b in value.split(128)]).clamp(min=ref.TINY) / 448
+                assert near(scales, want_scale, 12)
+                z = value / ref.f64(scales).repeat_interleave(128)[:n]
+                units, unit = ref.code_units(z)
+                r = torch.from_numpy(bits.astype(np.float64)) / 65536
+                low, high = (torch.floor(units + r + d) * unit for d in (-1e-4, 1e-4))
+                got = ref.f64(codes.float())
+                size = got.abs()
+                if value is not m:  # a root above zero stays above it
+                    low, high = (torch.where(value > 0, t.clamp(min=2.0 ** -9), t) for t in (low, high))
+                assert ((size == low.clamp(max=448)) | (size == high.clamp(max=448))).all()
+                assert ((got == 0) | (torch.sign(got) == torch.sign(value))).all()
+
+
+def test_adamw_8_bit_states_follow_their_means():
+    """Gradients of constant size: after 500 steps v is (1 - 0.999^500) g^2 = 0.39 g^2 and m is g.  A code's step is up to 1/8 of
+    its value and the roundings of 500 steps average out over 4096 elements: 5 % holds for both means with room; to nearest, v
+    would stop where 0.001 / 2 of its root's growth is half a step, below 0.02 g^2."""
+    params, grads = [torch.zeros(4096, device=DEV)], [torch.full((4096,), 0.5, device=DEV)]
+    opt = wd.AdamW(params, grads, state_bits=8, seed=3, lr=0.0, weight_decay=0.0)
+    for _ in range(500):
+        opt.step()
+    m = opt.exp_avg[0].float().view(-1, 128) * opt.avg_scale[0][:, None]
+    s = opt.exp_avg_sq[0].float().view(-1, 128) * opt.sq_scale[0][:, None]
+    assert abs(float(m.mean()) / 0.5 - 1) < 0.05 and abs(float((s * s).mean()) / (0.25 * (1 - 0.999 ** 500)) - 1) < 0.1
+
+
+def test_adamw_with_a_gradient_that_is_not_finite():
+    gen = generator(25)
+    params, grads = tensors_of(gen, [300, 50], F32)
+    grads[0][5], grads[0][200] = float("nan"), float("inf")
+    for bits in (32, 8):
+        copies = [p.clone() for p in params]
+        opt = wd.AdamW(copies, grads, state_bits=bits, **HYPER)
+        opt.step()
+        bad = ~copies[0].isfinite()
+        assert bad[5] and bad[200] and int(bad.sum()) == 2 and copies[1].isfinite().all()
+        if bits == 32:
+            assert not opt.exp_avg[0][5].isfinite() and int((~opt.exp_avg[0].isfinite()).sum()) == 2
+        else:
+            assert opt.exp_avg[0].float()[5].isnan() and opt.exp_avg[1].float().isfinite().all()
+            assert opt.avg_scale[0][0].isfinite() and opt.avg_scale[0][2].isfinite()
+
+
+def test_adamw_grad_scale_and_step_on_the_device():
+    gen = generator(26)
+    params, grads = tensors_of(gen, [700, 30], BF16)
+    masters = [p.float() for p in params]
+    for bits in (32, 8):
+        a = wd.AdamW([p.clone() for p in params], grads, masters=[m.clone() for m in masters], state_bits=bits, **HYPER)
+        b = wd.AdamW([p.clone() for p in params], [g.float() * 0.5 for g in grads], masters=[m.clone() for m in masters], state_bits=bits, **HYPER)
+        number = torch.zeros(1, dtype=torch.int64, device=DEV)
+        for _ in range(3):
+            number += 1
+            a.step(step_device=number, grad_scale=torch.tensor([0.5], device=DEV))
+            b.step()
+        for x, y in zip(a.masters, b.masters):
+            # the bias corrections come from another pow: a few roundings of updates no larger than 3 lr
+            assert ((ref.f64(x) - ref.f64(y)).abs() <= 3 * (3 * HYPER["lr"] * 16 * EPS24 + 2 * EPS24 * ref.f64(y).abs())).all()
+        if bits == 32:
+            assert all(torch.equal(x, y) for x, y in zip(a.exp_avg, b.exp_avg))
+
+
+# ---- streams, graphs, all of them together ---------------------------------------------------------
+def one_of_each(gen):
+    """Calls of every operator on inputs that stay, and a function that runs them and returns what they gave."""
+    x, r, w = normal(gen, 60, 200, dtype=BF16), normal(gen, 60, 200, dtype=BF16), 1 + 0.1 * normal(gen, 200)
+    b, b_scale = wd.quantise8(normal(gen, 300, 200))
+    p, q, d, u = drafts_of(gen, 20, 3, 6000, 1)
+    few = drafts_of(gen, 500, 1, 5, 0)
+    dy = normal(gen, 60, 200, dtype=BF16)
+    wide, wide_scale = wd.quantise8(normal(gen, 256, 4096))
+    one, one_scale = wd.quantise8(normal(gen, 4, 4096), rows=1)
+
+    def calls():
+        out = wd.rms_norm(x, w, residual=r, out8=E4M3)
+        dx, dw = wd.rms_norm_backward(dy, out.h, w, out.rstd)
+        return [out.h, out.q.view(torch.uint8), out.scale, out.rstd, dx, dw, wd.product8(out.q, out.scale, b, b_scale), wd.product8(one, one_scale, wide, wide_scale),
+                *wd.verify_drafts(p, q, d, u), *wd.verify_drafts(*few)]
+    return calls, (x, r, dy, u, few[3])
+
+
+def test_operators_on_another_stream():
+    calls, _ = one_of_each(generator(31))
+    want = [t.clone() for t in calls()]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = calls()
+    both = calls()  # and on two streams at once
+    torch.cuda.synchronize()
+    for a, b, c in zip(want, got, both):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_operators_in_a_graph_that_is_replayed():
+    gen = generator(32)
+    calls, changing = one_of_each(gen)
+    params, grads = tensors_of(gen, [500, 33], F32)
+    number = torch.zeros(1, dtype=torch.int64, device=DEV)
+    opt = wd.AdamW([p.clone() for p in params], grads, **HYPER)
+    eager = wd.AdamW([p.clone() for p in params], grads, **HYPER)
+    calls()
+    opt_state = [t for t in opt.params]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+        outs = calls()
+        number.add_(1)
+        opt.step(step_device=number)
+        graph.capture_end()
+    torch.cuda.current_stream().wait_stream(side)
+    for replay in range(4):
+        for t in changing[:3]:
+            t.copy_((torch.randn(t.shape, generator=gen)).to(t.dtype))
+        for t in changing[3:]:
+            t.copy_(torch.rand(t.shape, generator=gen))
+        grads[0].mul_(0.9)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        for a, b in zip(got, calls()):
+            assert torch.equal(a, b), replay
+        eager.step()
+        for a, b in zip(opt_state, eager.params):
+            assert ((ref.f64(a) - ref.f64(b)).abs() <= (replay + 1) * (3 * HYPER["lr"] * 16 * EPS24 + 2 * EPS24 * ref.f64(b).abs())).all(), replay
+        torch.cuda.synchronize()
+
+
+def test_zero_rows():
+    x = torch.empty((0, 40), dtype=BF16, device=DEV)
+    out = wd.rms_norm(x, None, residual=x, out8=E4M3)
+    assert out.q.shape == (0, 40) and out.scale.shape == (0, 1) and out.h.shape == (0, 40)
+    dx, dw = wd.rms_norm_backward(x, x, None, out.rstd)
+    assert dx.shape == (0, 40) and (dw == 0).all()
+    b, b_scale = wd.quantise8(torch.ones((30, 40), device=DEV))
+    assert wd.product8(out.q, out.scale, b, b_scale).shape == (0, 30)
+    a, a_scale = wd.quantise8(torch.ones((3, 40), device=DEV), rows=1)
+    assert wd.product8(a, a_scale, b[:0], b_scale[:0]).shape == (3, 0)
+    p = torch.empty((0, 2, 9), device=DEV)
+    accepted, tokens = wd.verify_drafts(p, p[:, :1], torch.empty((0, 1), dtype=torch.int32, device=DEV), torch.empty((0, 2), device=DEV))
+    assert accepted.shape == (0,) and tokens.shape == (0, 2)
+    wd.AdamW([torch.empty(0, device=DEV)], [torch.empty(0, device=DEV)]).step()
