@@ -120,7 +120,10 @@ int wdp_norm_backward(const wdp_norm_config* cfg, const wdp_norm_grad_buffers* b
  *   c[i][j] = sum over blocks b of 128 along k:
  *               a_scale[i][b] * b_scale[j / 128 or j][b] * sum over k in b of a[i][k] * b[j][k]
  * a is [m][k], b is [n][k] (a layer's weights as rows of outputs), both 8-bit; c is [m][n].
- * The sums within a block and over the blocks are float32, c is rounded once.  A NaN code or scale reaches the elements of its row or column. */
+ * c is rounded once.  The sums over the blocks are float32.  Within a block, a float32 c has
+ * float32 sums; for a 16-bit c the matrix core's 8-bit form adds the 128 products, off by about
+ * 2^-16 of the sum of their sizes (far below c's own rounding).  A NaN code or scale reaches the
+ * elements of its row or column and no others. */
 typedef struct wdp_product_config {
   uint32_t struct_size;   /* = sizeof(wdp_product_config)                                   */
   int32_t a_type, b_type; /* WDP_E4M3 or WDP_E5M2                                           */

@@ -158,7 +158,7 @@ template <typename P, typename G, bool EIGHT> __global__ __launch_bounds__(kThre
       most_m = fmaxf(most_m, fabsf(m[i]));
       most_s = fmaxf(most_s, v[i]);
     }
-    const float ms = fmaxf(group_max<16>(most_m), kTiny) / kLargestE4M3, vs = fmaxf(group_max<16>(most_s), kTiny) / kLargestE4M3;
+    const float ms = fmaxf(group_max<16>(most_m), kTiny) * (1.0f / kLargestE4M3), vs = fmaxf(group_max<16>(most_s), kTiny) * (1.0f / kLargestE4M3);
     if (n) {
       const uint64_t block = a.number[which] + uint64_t(at / WDP_BLOCK);
       const uint64_t four = block * (WDP_BLOCK / 4) + (at % WDP_BLOCK) / 4;

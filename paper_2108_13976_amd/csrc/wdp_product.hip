@@ -3,7 +3,7 @@
 // c[i][j] = sum over blocks b of a_scale[i][b] b_scale[.][b] (a block's inner product): one matrix instruction
 // 16 x 16 x 128 makes the inner products of a block, and one multiply-add an element adds them to the accumulators with
 // the scales' product.  The instruction is fed b as its first operand and a as its second, so that a lane holds ONE row
-// of a (one a_scale, and the block's scale product, per lane) and four adjacent columns of c (one store).
+// of a (one a_scale, and the block's scale product, per lane) and four adjacent columns of c.
 //
 // The order of k inside a block is the same for both operands and otherwise free: a lane takes the 16-byte chunks
 // g and g + 4 of its row (g = lane / 16).  In LDS a row is eight chunks; chunk c of row r lies at place c ^ (r / 2 % 8),
@@ -16,6 +16,8 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 struct ProductArgs {
   const uint8_t *a, *b;
@@ -24,83 +26,227 @@ struct ProductArgs {
   int64_t a_stride, b_stride, c_stride, as_row, as_block, bs_row, bs_block;
   int32_t m, n, k, blocks;  // blocks of 128 along k
   int32_t m_tiles, n_tiles;
+  int32_t aligned;          // rows of a and b start at 16-byte boundaries
+  int32_t by_row;           // b_scale has a row for each row of b, not for 128
 };
 
+// ---- a block's inner products ----------------------------------------------------------------------
+// The 8-bit matrix instruction sums a block's 128 products to about 16 bits (measured: 1.4e-5 of the result's size over
+// normal values, whatever the instruction's shape), which is far below the rounding of a 16-bit c.  A float32 c is worth
+// more than that: there the codes become bfloat16 first (exact: 8 significant bits hold 4) and four instructions
+// 16 x 16 x 32 sum their products in float32 (9e-9), at half the rate.
+template <bool EXACT> struct Fragment;  // a lane's 32 codes of a block
+template <> struct Fragment<false> {
+  i32x8 codes;
+};
+template <> struct Fragment<true> {
+  bf16x8 part[4];
+};
 
-template <int FA, int FB> __device__ __forceinline__ f32x4 inner(i32x8 b, i32x8 a) {
-  const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, zero, FB, FA, 0, 0, 0, 0);
+template <int F, bool EXACT> __device__ __forceinline__ Fragment<EXACT> fragment(i32x4 lo, i32x4 hi) {
+  Fragment<EXACT> f;
+  if constexpr (EXACT) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const i32x4 v = q < 2 ? lo : hi;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t w = uint32_t(v[2 * (q & 1) + h]);
+        const bf16x2 x = F == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, false);
+        const bf16x2 y = F == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, true);
+        f.part[q][4 * h] = x[0], f.part[q][4 * h + 1] = x[1], f.part[q][4 * h + 2] = y[0], f.part[q][4 * h + 3] = y[1];
+      }
+    }
+  } else {
+    f.codes = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  return f;
+}
+
+template <int FA, int FB, bool EXACT> __device__ __forceinline__ f32x4 inner(const Fragment<EXACT>& b, const Fragment<EXACT>& a) {
+  f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
+  if constexpr (EXACT) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.part[q], a.part[q], d, 0, 0, 0);
+    return d;
+  } else {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.codes, a.codes, d, FB, FA, 0, 0, 0, 0);
+  }
 }
 
 __device__ __forceinline__ int place(int row, int chunk) { return row * 8 + (chunk ^ ((row >> 1) & 7)); }
 
-// Chunk `chunk` (16 bytes) of a row's block; bytes from `left` on do not exist and read as zero.
-__device__ __forceinline__ i32x4 load_chunk(const uint8_t* row, int64_t at, int left) {
-  i32x4 v = {0, 0, 0, 0};
-  if (left >= 16) {
-    struct __attribute__((packed, aligned(1))) Raw {
-      i32x4 v;
-    };
-    return reinterpret_cast<const Raw*>(row + at)->v;
-  }
+// Column (from the tile's first) that row r of the staged b holds: of every 32 rows, 16 + 16 are dealt in fours to the
+// two instructions that follow each other, so that a lane's results of both are eight adjacent columns of c.
+__device__ __forceinline__ int column(int r) { return (r & ~31) | ((r & 12) << 1) | ((r & 16) >> 2) | (r & 3); }
+
+// The first `have` bytes of v (at most 16), zeros behind them.
+__device__ __forceinline__ i32x4 first_bytes(i32x4 v, int have) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (i < left) v[i >> 2] |= int(uint32_t(row[at + i]) << (8 * (i & 3)));
+  for (int d = 0; d < 4; ++d) {
+    const int bytes = have - 4 * d;
+    v[d] = bytes >= 4 ? v[d] : bytes <= 0 ? 0 : v[d] & ((1 << (8 * bytes)) - 1);
+  }
   return v;
 }
 
-template <typename C> __device__ __forceinline__ void store_c(const ProductArgs& p, int row, int col, f32x4 v) {
-  C* c = static_cast<C*>(p.c) + int64_t(row) * p.c_stride + col;
-  const float f[4] = {v[0], v[1], v[2], v[3]};
-  store_some<C, 4>(c, p.n - col, f);
+// Sixteen bytes of a row at `at`; those from `left` on do not exist and read as zero.  A chunk at a 16-byte boundary that
+// holds a byte of the row can be read whole (no page ends inside it).
+__device__ __forceinline__ i32x4 load_chunk(const uint8_t* row, int64_t at, int left, bool aligned) {
+  struct __attribute__((packed, aligned(1))) Raw {
+    i32x4 v;
+  };
+  if (left >= 16) return reinterpret_cast<const Raw*>(row + at)->v;
+  if (left <= 0) return i32x4{0, 0, 0, 0};
+  if (aligned) return first_bytes(reinterpret_cast<const Raw*>(row + at)->v, left);
+  uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+  for (int i = 0; i < left; ++i) {
+    const uint64_t byte = row[at + i];
+    if (i < 8) lo |= byte << (8 * i);
+    else hi |= byte << (8 * i - 64);
+  }
+  return i32x4{int(lo), int(lo >> 32), int(hi), int(hi >> 32)};
 }
 
-// A workgroup's tile of BM rows x BN columns, four waves of which each owns a part; the next block's chunks are
-// requested into registers before this block is multiplied, and go to the other half of LDS behind it.
-template <int FA, int FB, bool ROWS, typename C, int BM, int BN, int WAVES_M>
-__global__ __launch_bounds__(256) void product_tile_kernel(ProductArgs p) {
-  constexpr int WAVES_N = 4 / WAVES_M, TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;
-  constexpr int kA = BM * 8 / 256 ? BM * 8 / 256 : 1, kB = BN * 8 / 256;  // chunks a thread brings
-  __shared__ i32x4 lds_a[2][BM * 8], lds_b[2][BN * 8];
+// Results leave by way of LDS as whole 128-byte lines: a lane holds eight columns of a row, and a wave's store of such
+// pieces (64 bytes of sixteen rows) reaches memory at 2.6 TB/s, lines at more than 5.  A wave stages 32 of its rows x one
+// line; rows lie 144 bytes apart, which spreads the pieces of a quarter of a wave over the banks.
+constexpr int kLinePitch = 128 + 16, kLineBytes = 32 * kLinePitch;
+template <typename C> constexpr int kLineCols = 128 / sizeof(C);
+
+// The lane's eight columns (two instructions' results) of row 16 i + lane % 16, `pair`-th 32 columns of the line.
+template <typename C> __device__ __forceinline__ void put(uint8_t* mine, int lane, int i, int pair, f32x4 v, f32x4 w) {
+  const float f[8] = {v[0], v[1], v[2], v[3], w[0], w[1], w[2], w[3]};
+  union {
+    C c[8];
+    i32x4 v[sizeof(C) / 2];
+  } out;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) out.c[e] = from_float<C>(f[e]);
+#pragma unroll
+  for (int e = 0; e < int(sizeof(C) / 2); ++e)
+    *reinterpret_cast<i32x4*>(mine + (i * 16 + (lane & 15)) * kLinePitch + (pair * 32 + (lane >> 4) * 8) * int(sizeof(C)) + 16 * e) = out.v[e];
+}
+
+// The staged line to rows row0 .. row0 + 31, columns col0 ...  (A wave's own LDS accesses stay in order: the barriers
+// hold the compiler alone.)
+template <typename C> __device__ __forceinline__ void flush(const ProductArgs& p, const uint8_t* mine, int lane, int row0, int col0, int cols = kLineCols<C>) {
+  constexpr int kEach = 16 / sizeof(C);  // elements of a lane's store
+  struct __attribute__((packed, aligned(alignof(C)))) Raw {
+    i32x4 v;
+  };
+  __builtin_amdgcn_wave_barrier();
+  const int col = col0 + (lane & 7) * kEach, end = col0 + cols < p.n ? col0 + cols : p.n;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = i * 8 + (lane >> 3), row = row0 + r;
+    union {
+      i32x4 v;
+      C c[kEach];
+    } out;
+    out.v = *reinterpret_cast<const i32x4*>(mine + r * kLinePitch + (lane & 7) * 16);
+    if (row < p.m && col < end) {
+      C* c = static_cast<C*>(p.c) + int64_t(row) * p.c_stride + col;
+      if (col + kEach <= end) {
+        reinterpret_cast<Raw*>(c)->v = out.v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e)
+          if (col + e < end) c[e] = out.c[e];
+      }
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A wave's TM x TN results, whose first row and column are row0 and col0.
+template <typename C, int TM, int TN>
+__device__ __forceinline__ void store_tile(const ProductArgs& p, uint8_t* mine, int lane, int row0, int col0, const f32x4 (&acc)[TM][TN]) {
+  constexpr int kPairs = kLineCols<C> / 32;
+  static_assert(TN % 2 == 0 && TM % 2 == 0, "pairs of columns, 32 rows");
+#pragma unroll
+  for (int i = 0; i < TM; i += 2) {
+#pragma unroll
+    for (int j = 0; j < TN; j += 2 * kPairs) {
+      constexpr int kHere = TN / 2 < kPairs ? TN / 2 : kPairs;  // (a tile narrower than a line)
+#pragma unroll
+      for (int pair = 0; pair < kHere; ++pair)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) put<C>(mine, lane, h, pair, acc[i + h][j + 2 * pair], acc[i + h][j + 2 * pair + 1]);
+      flush<C>(p, mine, lane, row0 + i * 16, col0 + j * 16, kHere * 32);
+    }
+  }
+}
+
+// The tile of a workgroup.  Workgroups go to the eight XCDs in turn and each XCD has an L2 of its own: an XCD gets a
+// run of tiles, in bands of eight rows of tiles so that what it works on at a time shares both operands.
+__device__ __forceinline__ void tile_of(const ProductArgs& p, int* mt, int* nt) {
+  const int all = p.m_tiles * p.n_tiles, each = (all + 7) / 8, extra = all & 7;
+  const int x = blockIdx.x & 7, i = blockIdx.x >> 3;
+  const int tile = extra == 0 || x <= extra ? x * each + i : extra * each + (x - extra) * (each - 1) + i;
+  const int band = tile / (8 * p.n_tiles), in = tile % (8 * p.n_tiles);
+  const int high = p.m_tiles - band * 8 < 8 ? p.m_tiles - band * 8 : 8;
+  *mt = band * 8 + in % high;
+  *nt = in / high;
+}
+
+// ---- tiles ---------------------------------------------------------------------------------------------
+// A workgroup's tile of BM rows x BN columns, each of its waves TM x TN instructions of it.  The next block's chunks are
+// requested into registers before this block is multiplied, and go to the other half of LDS behind it: one barrier a
+// block, and any alignment, any k, rows beyond the last as zeros.
+template <int FA, int FB, typename C, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(ProductArgs p) {
+  constexpr bool EXACT = sizeof(C) == 4;
+  constexpr int kThreads = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+  constexpr int kA = BM * 8 / kThreads, kB = BN * 8 / kThreads;  // chunks a thread brings
+  static_assert(BM * 8 % kThreads == 0 && BN * 8 % kThreads == 0 && TN % 2 == 0 && BM + BN <= kThreads, "tile");
+  __shared__ i32x4 lds[2][(BM + BN) * 8];
+  static_assert(sizeof(lds) >= WM * WN * kLineBytes, "results are staged there");
   __shared__ __attribute__((aligned(16))) float scale_a[2][BM], scale_b[2][BN];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int64_t tile = blockIdx.x;
-  const int m0 = int(tile / p.n_tiles) * BM, n0 = int(tile % p.n_tiles) * BN;
-  const int wm = (wave % WAVES_M) * TM * 16, wn = (wave / WAVES_M) * TN * 16;
+  int mt, nt;
+  tile_of(p, &mt, &nt);
+  const int m0 = mt * BM, n0 = nt * BN;
+  const int wm = (wave % WM) * TM * 16, wn = (wave / WM) * TN * 16;
   const int r16 = lane & 15, g = lane >> 4;
 
   i32x4 next_a[kA], next_b[kB];
-  float next_sa = 0.0f, next_sb = 0.0f;
+  float next_s = 0.0f;
   auto request = [&](int block) {
     const int k0 = block * WDP_BLOCK;
 #pragma unroll
     for (int i = 0; i < kA; ++i) {
-      const int e = t + 256 * i, row = e >> 3, chunk = e & 7;
+      const int e = t + kThreads * i, row = e >> 3, chunk = e & 7;
       next_a[i] = i32x4{0, 0, 0, 0};
-      if (e < BM * 8 && m0 + row < p.m) next_a[i] = load_chunk(p.a + int64_t(m0 + row) * p.a_stride, k0 + chunk * 16, p.k - k0 - chunk * 16);
+      if (m0 + row < p.m) next_a[i] = load_chunk(p.a + int64_t(m0 + row) * p.a_stride, k0 + chunk * 16, p.k - k0 - chunk * 16, false);
     }
 #pragma unroll
     for (int i = 0; i < kB; ++i) {
-      const int e = t + 256 * i, row = e >> 3, chunk = e & 7;
+      const int e = t + kThreads * i, col = n0 + column(e >> 3), chunk = e & 7;
       next_b[i] = i32x4{0, 0, 0, 0};
-      if (n0 + row < p.n) next_b[i] = load_chunk(p.b + int64_t(n0 + row) * p.b_stride, k0 + chunk * 16, p.k - k0 - chunk * 16);
+      if (col < p.n) next_b[i] = load_chunk(p.b + int64_t(col) * p.b_stride, k0 + chunk * 16, p.k - k0 - chunk * 16, false);
     }
-    if (t < BM) next_sa = m0 + t < p.m ? p.a_scale[int64_t(m0 + t) * p.as_row + block * p.as_block] : 0.0f;
-    if (t < BN) next_sb = n0 + t < p.n ? p.b_scale[int64_t(ROWS ? n0 + t : (n0 + t) / WDP_BLOCK) * p.bs_row + block * p.bs_block] : 0.0f;
+    if (t < BM) {
+      next_s = m0 + t < p.m ? p.a_scale[int64_t(m0 + t) * p.as_row + block * p.as_block] : 0.0f;
+    } else if (t < BM + BN) {
+      const int col = n0 + column(t - BM);
+      next_s = col < p.n ? p.b_scale[int64_t(p.by_row ? col : col / WDP_BLOCK) * p.bs_row + block * p.bs_block] : 0.0f;
+    }
   };
   auto stage = [&](int half) {
 #pragma unroll
     for (int i = 0; i < kA; ++i) {
-      const int e = t + 256 * i;
-      if (e < BM * 8) lds_a[half][place(e >> 3, e & 7)] = next_a[i];
+      const int e = t + kThreads * i;
+      lds[half][place(e >> 3, e & 7)] = next_a[i];
     }
 #pragma unroll
     for (int i = 0; i < kB; ++i) {
-      const int e = t + 256 * i;
-      lds_b[half][place(e >> 3, e & 7)] = next_b[i];
+      const int e = t + kThreads * i;
+      lds[half][place(BM + (e >> 3), e & 7)] = next_b[i];
     }
-    if (t < BM) scale_a[half][t] = next_sa;
-    if (t < BN) scale_b[half][t] = next_sb;
+    if (t < BM) scale_a[half][t] = next_s;
+    else if (t < BM + BN) scale_b[half][t - BM] = next_s;
   };
 
   f32x4 acc[TM][TN];
@@ -115,66 +261,432 @@ __global__ __launch_bounds__(256) void product_tile_kernel(ProductArgs p) {
     const int half = block & 1;
     const bool more = block + 1 < p.blocks;
     if (more) request(block + 1);
-    i32x8 fa[TM];
-    float sa[TM];
+    Fragment<EXACT> fb[TN];
+    f32x4 sb[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int row = BM + wn + j * 16 + r16;
+      fb[j] = fragment<FB, EXACT>(lds[half][place(row, g)], lds[half][place(row, g + 4)]);
+      sb[j] = *reinterpret_cast<const f32x4*>(&scale_b[half][wn + j * 16 + g * 4]);
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int row = wm + i * 16 + r16;
-      const i32x4 lo = lds_a[half][place(row, g)], hi = lds_a[half][place(row, g + 4)];
-      fa[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      sa[i] = scale_a[half][row];
-    }
+      const Fragment<EXACT> fa = fragment<FA, EXACT>(lds[half][place(row, g)], lds[half][place(row, g + 4)]);
+      const float sa = scale_a[half][row];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int row = wn + j * 16 + r16;
-      const i32x4 lo = lds_b[half][place(row, g)], hi = lds_b[half][place(row, g + 4)];
-      const i32x8 fb = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      const f32x4 sb = *reinterpret_cast<const f32x4*>(&scale_b[half][wn + j * 16 + g * 4]);
+      for (int j = 0; j < TN; ++j) {
+        const f32x4 part = inner<FA, FB, EXACT>(fb[j], fa);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const f32x4 part = inner<FA, FB>(fb, fa[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[e], sa[i] * sb[e], acc[i][j][e]);
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[e], sa * sb[j][e], acc[i][j][e]);
       }
     }
     if (more) stage(half ^ 1);
     __syncthreads();
   }
+  store_tile<C>(p, reinterpret_cast<uint8_t*>(lds) + wave * kLineBytes, lane, m0 + wm, n0 + wn, acc);
+}
+
+// ---- large tiles -----------------------------------------------------------------------------------------
+// Rows at 16-byte boundaries: the chunks go from memory to LDS without registers between (a wave's instruction fills
+// 1 KB, eight rows; the lane that fills a place asks for the chunk that belongs there).  256 x 256 with eight waves of
+// 128 x 64: a block needs 2048 cycles of a SIMD's matrix core, 1536 of LDS for the fragments and 512 for the chunks.
+__device__ __forceinline__ void to_lds(const uint8_t* from, i32x4* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+template <int FA, int FB, bool ROWS, typename C, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_large_kernel(ProductArgs p) {
+  constexpr bool EXACT = sizeof(C) == 4;
+  constexpr int kWaves = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+  constexpr int kA = BM / 8 / kWaves, kB = BN / 8 / kWaves;  // eights of rows that a wave brings
+  __shared__ i32x4 lds[2][(BM + BN) * 8];
+  static_assert(sizeof(lds) >= kWaves * kLineBytes, "results are staged there");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int mt, nt;
+  tile_of(p, &mt, &nt);
+  // the last tile of rows ends with the last row: it computes some rows that its neighbour computes too, alike
+  const int m0 = mt * BM + BM <= p.m ? mt * BM : p.m - BM, n0 = nt * BN;
+  const int wm = (wave % WM) * TM * 16, wn = (wave / WM) * TN * 16;
+  const int r16 = lane & 15, g = lane >> 4;
+  // a lane's place in an eight of rows: row lane / 8, and the chunk that belongs at place lane % 8 of that row
+  const uint8_t* tile_a = p.a + int64_t(m0) * p.a_stride;
+  const uint8_t* tile_b = p.b + int64_t(n0) * p.b_stride;
+  uint32_t from_a[kA], from_b[kB];
+  int chunk_a[2], chunk_b[2];  // (in even and odd eights)
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int row = m0 + wm + i * 16 + r16;
-    if (row >= p.m) continue;
+  for (int i = 0; i < kA; ++i) {
+    const int row = (wave * kA + i) * 8 + (lane >> 3);
+    chunk_a[i & 1] = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    from_a[i] = uint32_t(row) * uint32_t(p.a_stride) + chunk_a[i & 1];
+  }
+#pragma unroll
+  for (int i = 0; i < kB; ++i) {
+    const int row = (wave * kB + i) * 8 + (lane >> 3), col = column(row);
+    chunk_b[i & 1] = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    from_b[i] = uint32_t(n0 + col < p.n ? col : p.n - 1 - n0) * uint32_t(p.b_stride) + chunk_b[i & 1];
+  }
+  const float* tile_sa = p.a_scale + int64_t(m0 + wm) * p.as_row;
+  const uint32_t from_sa = uint32_t(r16) * uint32_t(p.as_row);
+  // scales of b: one for the wave's columns, or (ROWS) one for each column of the lane's results
+  const float* from_sb[ROWS ? TN : 1][ROWS ? 4 : 1];
+  float next_sa[TM], next_sb[ROWS ? TN : 1][ROWS ? 4 : 1];
+#pragma unroll
+  for (int j = 0; j < (ROWS ? TN : 1); ++j)
+#pragma unroll
+    for (int e = 0; e < (ROWS ? 4 : 1); ++e) {
+      const int col = n0 + wn + (ROWS ? column(j * 16 + g * 4 + e) : 0), at = col < p.n ? col : p.n - 1;
+      from_sb[j][e] = p.b_scale + int64_t(ROWS && p.by_row ? at : at / WDP_BLOCK) * p.bs_row;
+    }
+  auto request = [&](int block, int half) {
+    const int k0 = block * WDP_BLOCK;
+#pragma unroll
+    for (int j = 0; j < (ROWS ? TN : 1); ++j)
+#pragma unroll
+      for (int e = 0; e < (ROWS ? 4 : 1); ++e) next_sb[j][e] = from_sb[j][e][block * p.bs_block];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) next_sa[i] = (tile_sa + block * p.as_block + i * 16 * p.as_row)[from_sa];
+    const uint8_t *a = tile_a + k0, *b = tile_b + k0;
+    if (k0 + WDP_BLOCK <= p.k) {
+#pragma unroll
+      for (int i = 0; i < kA; ++i) to_lds(a + from_a[i], &lds[half][(wave * kA + i) * 64]);
+#pragma unroll
+      for (int i = 0; i < kB; ++i) to_lds(b + from_b[i], &lds[half][BM * 8 + (wave * kB + i) * 64]);
+    } else {
+      // the last block's end: chunks with nothing of the row stay out (what they hold is cleared below)
+#pragma unroll
+      for (int i = 0; i < kA; ++i)
+        if (k0 + chunk_a[i & 1] < p.k) to_lds(a + from_a[i], &lds[half][(wave * kA + i) * 64]);
+#pragma unroll
+      for (int i = 0; i < kB; ++i)
+        if (k0 + chunk_b[i & 1] < p.k) to_lds(b + from_b[i], &lds[half][BM * 8 + (wave * kB + i) * 64]);
+    }
+  };
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  request(0, 0);
+  for (int block = 0; block < p.blocks; ++block) {
+    const int half = block & 1;
+    float sa[TM], sb[ROWS ? TN : 1][ROWS ? 4 : 1];  // (without ROWS both are in sa)
+    __syncthreads();  // this block's chunks have arrived, and everyone is through with the other half
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = ROWS ? next_sa[i] : next_sa[i] * next_sb[0][0];
+#pragma unroll
+    for (int j = 0; j < (ROWS ? TN : 1); ++j)
+#pragma unroll
+      for (int e = 0; e < (ROWS ? 4 : 1); ++e) sb[j][e] = next_sb[j][e];
+    if (block + 1 < p.blocks) request(block + 1, half ^ 1);
+    else if (p.k & (WDP_BLOCK - 1)) {
+      // bytes beyond k: zeros
+      const int left = p.k & (WDP_BLOCK - 1);
+      for (int e = threadIdx.x; e < (BM + BN) * 8; e += 64 * kWaves) {
+        const int have = left - (e & 7) * 16;
+        if (have < 16) {
+          i32x4* at = lds[half] + place(e >> 3, e & 7);
+          *at = first_bytes(*at, have);
+        }
+      }
+      __syncthreads();
+    }
+    Fragment<EXACT> fb[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      const int col = n0 + wn + j * 16 + g * 4;
-      if (col < p.n) store_c<C>(p, row, col, acc[i][j]);
+      const int row = BM + wn + j * 16 + r16;
+      fb[j] = fragment<FB, EXACT>(lds[half][place(row, g)], lds[half][place(row, g + 4)]);
+    }
+    auto load_a = [&](int i) {
+      const int row = wm + i * 16 + r16;
+      return fragment<FA, EXACT>(lds[half][place(row, g)], lds[half][place(row, g + 4)]);
+    };
+    constexpr int kDelay = 3;
+    // an instruction's results are added kDelay instructions later: the matrix core goes on meanwhile
+    Fragment<EXACT> fa[2];
+    fa[0] = load_a(0);
+    f32x4 part[kDelay + 1];
+#pragma unroll
+    for (int e = 0; e < TM * TN + kDelay; ++e) {
+      if (e < TM * TN) {
+        const int i = e / TN;
+        if (e % TN == 0 && i + 1 < TM) fa[(i + 1) & 1] = load_a(i + 1);
+        part[e % (kDelay + 1)] = inner<FA, FB, EXACT>(fb[e % TN], fa[i & 1]);
+      }
+      if (e >= kDelay) {
+        const int d = e - kDelay;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) acc[d / TN][d % TN][x] = fmaf(part[d % (kDelay + 1)][x], ROWS ? sa[d / TN] * sb[ROWS ? d % TN : 0][ROWS ? x : 0] : sa[d / TN], acc[d / TN][d % TN][x]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  __syncthreads();
+  store_tile<C>(p, reinterpret_cast<uint8_t*>(lds) + wave * kLineBytes, lane, m0 + wm, n0 + wn, acc);
+}
+
+// ---- few rows --------------------------------------------------------------------------------------------
+// b is streamed once, straight into registers: a workgroup owns 16 TN columns and 16 TM rows, its waves take the blocks of
+// k in turn, DEPTH of them requested at a time, and join their sums in LDS.
+template <int FA, int FB, typename C, int TM, int TN, int WAVES, int DEPTH>
+__global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs p) {
+  constexpr bool EXACT = sizeof(C) == 4;
+  __shared__ f32x4 sums[WAVES][TM][TN][64];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r16 = lane & 15, g = lane >> 4;
+  const int n0 = blockIdx.x * 16 * TN, m0 = blockIdx.y * 16 * TM;
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  // rows and columns beyond the last read the last one: their results are not stored
+  const uint8_t *a[TM], *b[TN];
+  const float *as[TM], *bs[TN][4];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int row = m0 + i * 16 + r16 < p.m ? m0 + i * 16 + r16 : p.m - 1;
+    a[i] = p.a + int64_t(row) * p.a_stride + g * 16;
+    as[i] = p.a_scale + int64_t(row) * p.as_row;
+  }
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int col = n0 + j * 16 + r16 < p.n ? n0 + j * 16 + r16 : p.n - 1;
+    b[j] = p.b + int64_t(col) * p.b_stride + g * 16;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {  // of the lane's results
+      const int at = n0 + j * 16 + g * 4 + e < p.n ? n0 + j * 16 + g * 4 + e : p.n - 1;
+      bs[j][e] = p.b_scale + int64_t(p.by_row ? at : at / WDP_BLOCK) * p.bs_row;
+    }
+  }
+  struct __attribute__((packed, aligned(1))) Raw {
+    i32x4 v;
+  };
+  i32x4 la[DEPTH][TM][2], lb[DEPTH][TN][2];
+  float sa[DEPTH][TM], sb[DEPTH][TN][4];
+  auto scales = [&](int d, int block) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[d][i] = as[i][block * p.as_block];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      sb[d][j][0] = bs[j][0][block * p.bs_block];
+#pragma unroll
+      for (int e = 1; e < 4; ++e) sb[d][j][e] = p.by_row ? bs[j][e][block * p.bs_block] : sb[d][j][0];
+    }
+  };
+  auto add = [&](int d) {
+    Fragment<EXACT> fb[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fb[j] = fragment<FB, EXACT>(lb[d][j][0], lb[d][j][1]);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const Fragment<EXACT> fa = fragment<FA, EXACT>(la[d][i][0], la[d][i][1]);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const f32x4 part = inner<FA, FB, EXACT>(fb[j], fa);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[e], sa[d][i] * sb[d][j][e], acc[i][j][e]);
+      }
+    }
+  };
+  const int whole = p.k / WDP_BLOCK;  // blocks of 128; what is left of k is one more, and a wave's of its own
+  int block = wave;
+  for (; block + (DEPTH - 1) * WAVES < whole; block += DEPTH * WAVES) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      const int64_t k0 = int64_t(block + d * WAVES) * WDP_BLOCK;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) lb[d][j][0] = reinterpret_cast<const Raw*>(b[j] + k0)->v, lb[d][j][1] = reinterpret_cast<const Raw*>(b[j] + k0 + 64)->v;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) la[d][i][0] = reinterpret_cast<const Raw*>(a[i] + k0)->v, la[d][i][1] = reinterpret_cast<const Raw*>(a[i] + k0 + 64)->v;
+      scales(d, block + d * WAVES);
+    }
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) add(d);
+  }
+  for (; block < p.blocks; block += WAVES) {
+    const int k0 = block * WDP_BLOCK, left = p.k - k0 - g * 16;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) lb[0][j][0] = load_chunk(b[j], k0, left, p.aligned), lb[0][j][1] = load_chunk(b[j], k0 + 64, left - 64, p.aligned);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) la[0][i][0] = load_chunk(a[i], k0, left, p.aligned), la[0][i][1] = load_chunk(a[i], k0 + 64, left - 64, p.aligned);
+    scales(0, block);
+    add(0);
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sums[wave][i][j][lane] = acc[i][j];
+  __syncthreads();
+  for (int e = wave; e < TM * TN; e += WAVES) {
+    const int i = e / TN, j = e % TN, row = m0 + i * 16 + r16, col = n0 + j * 16 + g * 4;
+    f32x4 total = sums[0][i][j][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) total += sums[w][i][j][lane];
+    if (row < p.m && col < p.n) {
+      const float f[4] = {total[0], total[1], total[2], total[3]};
+      store_some<C, 4>(static_cast<C*>(p.c) + int64_t(row) * p.c_stride + col, p.n - col, f);
     }
   }
 }
 
-// (a launch takes up to 2^22 tiles: all sizes of a grid, and rows counted in 32 bits, stay far from their limits)
-template <int FA, int FB, bool ROWS, typename C> void launch(ProductArgs p, hipStream_t stream) {
-  const int64_t rows = p.m;
-  p.n_tiles = (p.n + 127) / 128;
-  const int64_t most = (int64_t(1) << 22) / p.n_tiles * 128;
+// ---- b in LDS ----------------------------------------------------------------------------------------------
+// Many rows against a b that LDS holds whole (PN columns, all of k): staged once, then each wave goes through its own
+// tiles of 32 rows without a barrier, a straight from memory into registers, the next tile's requested before this one's
+// results leave.  Memory bounds it: a is read once and c written once.
+template <int FA, int FB, typename C, int PN, int KB>
+__global__ __launch_bounds__(512) void product_panel_kernel(ProductArgs p) {
+  constexpr bool EXACT = sizeof(C) == 4;
+  constexpr int kCols = kLineCols<C>, kPairs = kCols / 32;
+  __shared__ i32x4 lds_b[KB][PN * 8];
+  __shared__ __attribute__((aligned(16))) float scale_b[KB][PN];
+  __shared__ __attribute__((aligned(16))) uint8_t staged[8][kLineBytes];
+  const int t = threadIdx.x, lane = t & 63, r16 = lane & 15, g = lane >> 4;
+  const int n0 = blockIdx.y * PN;
+  for (int e = t; e < KB * PN * 8; e += 512) {
+    const int block = e / (PN * 8), row = e / 8 % PN, chunk = e & 7, col = n0 + column(row), k0 = block * WDP_BLOCK + chunk * 16;
+    lds_b[block][place(row, chunk)] = col < p.n ? load_chunk(p.b + int64_t(col) * p.b_stride, k0, p.k - k0, p.aligned) : i32x4{0, 0, 0, 0};
+  }
+  for (int e = t; e < KB * PN; e += 512) {
+    const int block = e / PN, row = e % PN, col = n0 + column(row);
+    scale_b[block][row] = col < p.n && block < p.blocks ? p.b_scale[int64_t(p.by_row ? col : col / WDP_BLOCK) * p.bs_row + block * p.bs_block] : 0.0f;
+  }
+  __syncthreads();
+  uint8_t* mine = staged[t >> 6];
+  const int step = gridDim.x * 8;
+  int tile = blockIdx.x * 8 + (t >> 6);
+  i32x4 lo[2][KB], hi[2][KB];
+  float sa[2][KB];
+  auto request = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = tile * 32 + i * 16 + r16 < p.m ? tile * 32 + i * 16 + r16 : p.m - 1;
+      const uint8_t* a = p.a + int64_t(row) * p.a_stride;
+#pragma unroll
+      for (int q = 0; q < KB; ++q) {
+        const int k0 = q * WDP_BLOCK + g * 16;
+        lo[i][q] = load_chunk(a, k0, p.k - k0, p.aligned);
+        hi[i][q] = load_chunk(a, k0 + 64, p.k - k0 - 64, p.aligned);
+        sa[i][q] = q < p.blocks ? p.a_scale[int64_t(row) * p.as_row + q * p.as_block] : 0.0f;
+      }
+    }
+  };
+  if (tile < p.m_tiles) request(tile);
+  for (; tile < p.m_tiles; tile += step) {
+    Fragment<EXACT> fa[2][KB];
+    float s[2][KB];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int q = 0; q < KB; ++q) fa[i][q] = fragment<FA, EXACT>(lo[i][q], hi[i][q]), s[i][q] = sa[i][q];
+    if (tile + step < p.m_tiles) request(tile + step);
+#pragma unroll
+    for (int line = 0; line < PN / kCols; ++line) {
+      const int c0 = n0 + line * kCols;
+      if (c0 >= p.n) break;
+#pragma unroll
+      for (int pair = 0; pair < kPairs; ++pair) {
+        f32x4 acc[2][2];
+#pragma unroll
+        for (int q = 0; q < KB; ++q) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int first = line * kCols + pair * 32 + h * 16, row = first + r16;
+            const Fragment<EXACT> fb = fragment<FB, EXACT>(lds_b[q][place(row, g)], lds_b[q][place(row, g + 4)]);
+            const f32x4 sb = *reinterpret_cast<const f32x4*>(&scale_b[q][first + g * 4]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const f32x4 part = inner<FA, FB, EXACT>(fb, fa[i][q]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[i][h][e] = q == 0 ? part[e] * (s[i][q] * sb[e]) : fmaf(part[e], s[i][q] * sb[e], acc[i][h][e]);
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) put<C>(mine, lane, i, pair, acc[i][0], acc[i][1]);
+      }
+      flush<C>(p, mine, lane, tile * 32, c0);
+    }
+  }
+}
+
+template <int FA, int FB, typename C, int BM, int BN, int WM, int WN> void launch_tiles(ProductArgs p, hipStream_t stream) {
+  p.m_tiles = (p.m + BM - 1) / BM;
+  p.n_tiles = (p.n + BN - 1) / BN;
+  product_tile_kernel<FA, FB, C, BM, BN, WM, WN><<<dim3(unsigned(p.m_tiles) * unsigned(p.n_tiles)), dim3(64 * WM * WN), 0, stream>>>(p);
+}
+template <int FA, int FB, bool ROWS, typename C, int BM, int BN, int WM, int WN> void launch_large(ProductArgs p, hipStream_t stream) {
+  p.m_tiles = (p.m + BM - 1) / BM;
+  p.n_tiles = (p.n + BN - 1) / BN;
+  product_large_kernel<FA, FB, ROWS, C, BM, BN, WM, WN><<<dim3(unsigned(p.m_tiles) * unsigned(p.n_tiles)), dim3(64 * WM * WN), 0, stream>>>(p);
+}
+template <int FA, int FB, typename C, int TM, int TN, int WAVES, int DEPTH> void launch_stream(const ProductArgs& p, hipStream_t stream) {
+  product_stream_kernel<FA, FB, C, TM, TN, WAVES, DEPTH>
+      <<<dim3(unsigned((p.n + 16 * TN - 1) / (16 * TN)), unsigned((p.m + 16 * TM - 1) / (16 * TM))), dim3(64 * WAVES), 0, stream>>>(p);
+}
+template <int FA, int FB, typename C, int PN, int KB> void launch_panel(ProductArgs p, hipStream_t stream) {
+  p.m_tiles = (p.m + 31) / 32;
+  const int panels = (p.n + PN - 1) / PN, groups = (p.m_tiles + 7) / 8, most = 512 / panels;
+  product_panel_kernel<FA, FB, C, PN, KB><<<dim3(unsigned(groups < most ? groups : most > 0 ? most : 1), unsigned(panels)), dim3(512), 0, stream>>>(p);
+}
+
+// Which kernel, by sizes and alignment (us on this card; k in blocks of 128).
+//   - Many rows against up to 64 columns and 256 of k: b in LDS.  2000000 x 5 x 64: 38 against 108 in tiles of 64;
+//     300000 x 47 x 200: 26 against 28; 10000 x 5 x 300 would take 8.7 against 5.2, hence the bound on m.
+//   - Up to 128 tiles of 64 x 64 (a launch of tiles would leave half the chip idle through all of k): b streamed, in the
+//     largest piece of c that still makes 240 workgroups.  128 x 4096 x 4096: 15 against 20; 700 x 700 x 3000: 10 against 16;
+//     beyond, 200 x 4096 x 4096: 28 against 21.  With k of one or two blocks there is nothing to stream: 2000 x 256 x 128
+//     takes 4.0 against 3.2, so only up to 32 tiles there (300 x 200 x 256: 2.8 against 3.6).
+//   - Rows that do not start at 16-byte boundaries: tiles by way of registers.
+//   - Else the tiles that need the least time for a block of k: rounds of 256 tiles of 256 x 256 at 2.1, 512 of 128 x 128
+//     at 1.2 (1.0 with one tile a CU at most), 1024 of 64 x 64 at 1.5 (0.95, 0.65 with two, one a CU); exact ones 2.0 and
+//     1.5.  4096^3: 67 against 75 and (64) 100; 2048 x 2048 x 2000: 35, 19, 25; 1000^3: 19, 10.5, 8.3.  Columns up to 64
+//     leave half of a wider tile empty: 500000 x 64 x 300 takes 58 against 50.
+template <int FA, int FB, typename C> void launch_slice(const ProductArgs& p, hipStream_t stream) {
+  constexpr bool EXACT = sizeof(C) == 4;
+  const auto tiles = [&](int64_t m, int64_t n) { return (p.m + m - 1) / m * ((p.n + n - 1) / n); };
+  const auto rounds = [](int64_t tiles, int at_once) { return double((tiles + at_once - 1) / at_once); };
+  const int64_t t64 = tiles(64, 64);
+  if (p.n <= 64 && p.blocks <= 2 && p.m >= 16384) {
+    if (p.blocks == 1) return launch_panel<FA, FB, C, 64, 1>(p, stream);
+    return launch_panel<FA, FB, C, 64, 2>(p, stream);
+  }
+  if (t64 <= 128 && (p.blocks > 2 || t64 <= 32)) {
+    if (tiles(64, 32) >= 240) return launch_stream<FA, FB, C, 4, 2, 8, 1>(p, stream);
+    if (tiles(32, 32) >= 240) return launch_stream<FA, FB, C, 2, 2, 8, 2>(p, stream);
+    if (tiles(32, 16) >= 240) return launch_stream<FA, FB, C, 2, 1, 8, 2>(p, stream);
+    return launch_stream<FA, FB, C, 1, 1, 8, 4>(p, stream);
+  }
+  // (places in a tile are 32-bit offsets from its first row)
+  const bool near = p.a_stride <= (1 << 23) && p.b_stride <= (1 << 23) && p.as_row <= (1 << 27);
+  if (!p.aligned || !near || p.m < 64) return launch_tiles<FA, FB, C, 128, 128, 2, 2>(p, stream);
+  const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
+  double cost64 = t64 <= 256 ? 0.65 : t64 <= 512 ? 0.95 : 1.5 * rounds(t64, 1024);
+  const double cost128 = t128 <= 256 ? 1.0 : (EXACT ? 2.0 : 1.17) * rounds(t128, 512), cost256 = 2.1 * rounds(t256, 256);
+  if (p.n <= 64) cost64 = 0.0;
+  if constexpr (!EXACT) {
+    if (!p.by_row && p.m >= 256 && cost256 < cost128 && cost256 < cost64) return launch_large<FA, FB, false, C, 256, 256, 2, 4>(p, stream);
+    if (p.by_row && p.m >= 128 && cost128 < cost64) return launch_large<FA, FB, true, C, 128, 128, 2, 2>(p, stream);
+  }
+  if (!p.by_row && p.m >= 128 && cost128 < cost64) return launch_large<FA, FB, false, C, 128, 128, 2, 2>(p, stream);
+  launch_large<FA, FB, true, C, 64, 64, 2, 2>(p, stream);
+}
+
+// (a launch takes up to 2^22 tiles of 128 x 128: all sizes of a grid, and rows counted in 32 bits, stay far from their limits)
+template <int FA, int FB, typename C> void launch(const ProductArgs& p, hipStream_t stream) {
+  const int64_t rows = p.m, most = (int64_t(1) << 22) / ((p.n + 127) / 128) * 128;
   for (int64_t at = 0; at < rows; at += most) {
     ProductArgs q = p;
     q.a += at * p.a_stride;
     q.a_scale += at * p.as_row;
     q.c = static_cast<C*>(p.c) + at * p.c_stride;
     q.m = int32_t(rows - at < most ? rows - at : most);
-    q.m_tiles = (q.m + 127) / 128;
-    product_tile_kernel<FA, FB, ROWS, C, 128, 128, 2><<<dim3(unsigned(int64_t(q.m_tiles) * q.n_tiles)), dim3(256), 0, stream>>>(q);
+    launch_slice<FA, FB, C>(q, stream);
   }
 }
-template <int FA, int FB, bool ROWS> void launch_c(const ProductArgs& p, int c_type, hipStream_t stream) {
-  if (c_type == WDP_F32) launch<FA, FB, ROWS, float>(p, stream);
-  else if (c_type == WDP_BF16) launch<FA, FB, ROWS, bf16>(p, stream);
-  else launch<FA, FB, ROWS, f16>(p, stream);
-}
-template <int FA, int FB> void launch_rows(const ProductArgs& p, bool rows, int c_type, hipStream_t stream) {
-  if (rows) launch_c<FA, FB, true>(p, c_type, stream);
-  else launch_c<FA, FB, false>(p, c_type, stream);
+template <int FA, int FB> void launch_c(const ProductArgs& p, int c_type, hipStream_t stream) {
+  if (c_type == WDP_F32) launch<FA, FB, float>(p, stream);
+  else if (c_type == WDP_BF16) launch<FA, FB, bf16>(p, stream);
+  else launch<FA, FB, f16>(p, stream);
 }
 
 int check(const wdp_product_config& c) {
@@ -211,13 +723,13 @@ int wdp_product(const wdp_product_config* cfg, const wdp_product_buffers* b) {
   if (!aligned(b->a_scale, 4) || !aligned(b->b_scale, 4) || !aligned(b->c, size_of(cfg->c_type)) || !aligned(b->workspace, 256)) return WD_E_ALIGN;
   const ProductArgs p = {static_cast<const uint8_t*>(b->a), static_cast<const uint8_t*>(b->b), b->a_scale, b->b_scale, b->c, cfg->a_stride, cfg->b_stride,
                          cfg->c_stride, cfg->a_scale_row_stride, cfg->a_scale_block_stride, cfg->b_scale_row_stride, cfg->b_scale_block_stride,
-                         int32_t(cfg->m), cfg->n, cfg->k, (cfg->k + WDP_BLOCK - 1) / WDP_BLOCK, 0, 0};
+                         int32_t(cfg->m), cfg->n, cfg->k, (cfg->k + WDP_BLOCK - 1) / WDP_BLOCK, 0, 0,
+                         aligned(b->a, 16) && aligned(b->b, 16) && cfg->a_stride % 16 == 0 && cfg->b_stride % 16 == 0, cfg->b_scale_rows == 1};
   const hipStream_t stream = static_cast<hipStream_t>(cfg->stream);
-  const bool rows = cfg->b_scale_rows == 1;
-  if (cfg->a_type == WDP_E4M3 && cfg->b_type == WDP_E4M3) launch_rows<0, 0>(p, rows, cfg->c_type, stream);
-  else if (cfg->a_type == WDP_E4M3) launch_rows<0, 1>(p, rows, cfg->c_type, stream);
-  else if (cfg->b_type == WDP_E4M3) launch_rows<1, 0>(p, rows, cfg->c_type, stream);
-  else launch_rows<1, 1>(p, rows, cfg->c_type, stream);
+  if (cfg->a_type == WDP_E4M3 && cfg->b_type == WDP_E4M3) launch_c<0, 0>(p, cfg->c_type, stream);
+  else if (cfg->a_type == WDP_E4M3) launch_c<0, 1>(p, cfg->c_type, stream);
+  else if (cfg->b_type == WDP_E4M3) launch_c<1, 0>(p, cfg->c_type, stream);
+  else launch_c<1, 1>(p, cfg->c_type, stream);
   return launched();
 }
 

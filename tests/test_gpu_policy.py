@@ -200,15 +200,18 @@ def operands(gen, m, n, k, a_type=E4M3, b_type=E4M3, by_row=False):
 
 
 def check_product(a, a_scale, b, b_scale, by_row, c):
-    """A block's 128 products are exact in float32 (8 significant bits); 127 adds in whatever order, each off by a step at
-    most (an adder that truncates), then two operations a block with the scales."""
+    """A block's 128 products are exact in float32 (8 significant bits); float32 c: 127 adds in whatever order, each off by a
+    step at most (an adder that truncates), then two operations a block with the scales.  16-bit c: the adder's 2^-16 of the
+    sum of the products' sizes (documented) instead."""
     want, size = ref.product(a, a_scale, b, b_scale, by_row)
     blocks = a_scale.shape[1]
-    assert ((ref.f64(c) - want).abs() <= (2 * 127 + 2 * blocks + 4) * EPS24 * size + ref.rounding(want, c.dtype) * 1.01 + 1e-38).all()
+    adder = 2 * 127 * EPS24 if c.dtype == F32 else 2.0 ** -16
+    assert ((ref.f64(c) - want).abs() <= (adder + (2 * blocks + 4) * EPS24) * size + ref.rounding(want, c.dtype) * 1.01 + 1e-38).all()
 
 
 SIZES = [(1, 1, 1), (1, 5, 21), (2, 3, 127), (5, 128, 128), (16, 17, 129), (17, 16, 255), (50, 256, 256), (33, 129, 1000), (64, 64, 64), (100, 333, 384),
-         (129, 127, 130), (200, 40, 2048), (257, 300, 515), (1000, 5, 64), (1, 4096, 512), (7, 1000, 4096), (16, 130, 16384), (300, 513, 1024), (512, 512, 640)]
+         (129, 127, 130), (200, 40, 2048), (257, 300, 515), (1000, 5, 64), (1, 4096, 512), (7, 1000, 4096), (16, 130, 16384), (300, 513, 1024), (512, 512, 640),
+         (700, 700, 1100), (130, 2000, 400), (2000, 64, 900), (70, 4000, 260), (40, 4000, 2050), (20, 5000, 390)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
@@ -221,7 +224,9 @@ def test_product_against_float64(m, n, k, a_type, b_type, by_row, dtype):
     check_product(a, a_scale, b, b_scale, by_row and n != -(-n // 128), wd.product8(a, a_scale, b, b_scale, dtype=dtype))
 
 
-@pytest.mark.parametrize("m,n,k,by_row", [(2048, 1024, 512, False), (2100, 1000, 700, False), (4096, 256, 256, False), (5003, 256, 256, False), (3000, 200, 200, True), (1500, 1537, 1100, True)])
+@pytest.mark.parametrize("m,n,k,by_row", [(2048, 1024, 512, False), (2100, 1000, 700, False), (4096, 256, 256, False), (5003, 256, 256, False), (3000, 200, 200, True), (1500, 1537, 1100, True),
+                                           (16384, 5, 21, False), (16385, 64, 128, False), (20001, 47, 200, True), (16400, 33, 256, False), (17000, 64, 257, False), (2050, 8192, 300, False),
+                                           (4097, 4096, 130, False), (4100, 2050, 150, True), (9000, 300, 300, False)])
 def test_product_of_many_rows(m, n, k, by_row):
     gen = generator(m, n, k)
     args = operands(gen, m, n, k, by_row=by_row)
