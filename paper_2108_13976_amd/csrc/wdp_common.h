@@ -31,24 +31,63 @@ inline int launched() {
 template <typename T> __device__ __forceinline__ float to_float(T v) { return static_cast<float>(v); }
 template <typename T> __device__ __forceinline__ T from_float(float v) { return static_cast<T>(v); }
 
-// N elements at p (any alignment that the elements have) as floats.  Global memory takes a 16-byte access at any
-// address, so whole vectors need no aligned rows.
+// N adjacent elements at p (any alignment that the elements have) as floats, and back, in accesses of sixteen bytes: global
+// memory takes those at any address, so whole vectors need no aligned rows.  (A struct of elements would be split into
+// whatever pieces the compiler likes, hence the words.)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <typename V> struct __attribute__((packed, aligned(1))) Unaligned {
+  V v;
+};
+template <typename V> __device__ __forceinline__ V load_raw(const void* p) { return static_cast<const Unaligned<V>*>(p)->v; }
+template <typename V> __device__ __forceinline__ void store_raw(void* p, V v) { static_cast<Unaligned<V>*>(p)->v = v; }
+
+template <typename T> __device__ __forceinline__ void widen(uint32_t w, float v[2]);
+template <> __device__ __forceinline__ void widen<bf16>(uint32_t w, float v[2]) { v[0] = __uint_as_float(w << 16), v[1] = __uint_as_float(w & 0xFFFF0000u); }
+template <> __device__ __forceinline__ void widen<f16>(uint32_t w, float v[2]) {
+  typedef f16 f16x2 __attribute__((ext_vector_type(2)));
+  const f16x2 h = __builtin_bit_cast(f16x2, w);
+  v[0] = float(h[0]), v[1] = float(h[1]);
+}
+template <typename T> __device__ __forceinline__ uint32_t narrow(float a, float b) {
+  typedef T Tx2 __attribute__((ext_vector_type(2)));
+  const Tx2 h = {static_cast<T>(a), static_cast<T>(b)};
+  return __builtin_bit_cast(uint32_t, h);
+}
+
 template <typename T, int N> __device__ __forceinline__ void load_vec(const T* __restrict__ p, float v[N]) {
-  struct __attribute__((packed, aligned(alignof(T)))) Raw {
-    T e[N];
-  };
-  const Raw raw = *reinterpret_cast<const Raw*>(p);
+  if constexpr (sizeof(T) == 4) {
+    static_assert(N % 4 == 0, "whole accesses");
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = to_float<T>(raw.e[i]);
+    for (int i = 0; i < N; i += 4) {
+      const u32x4 w = load_raw<u32x4>(p + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i + e] = __uint_as_float(w[e]);
+    }
+  } else if constexpr (N % 8 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) {
+      const u32x4 w = load_raw<u32x4>(p + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) widen<T>(w[e], v + i + 2 * e);
+    }
+  } else {
+    static_assert(N == 4, "whole accesses");
+    const u32x2 w = load_raw<u32x2>(p);
+    widen<T>(w[0], v), widen<T>(w[1], v + 2);
+  }
 }
 template <typename T, int N> __device__ __forceinline__ void store_vec(T* __restrict__ p, const float v[N]) {
-  struct __attribute__((packed, aligned(alignof(T)))) Raw {
-    T e[N];
-  };
-  Raw raw;
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) raw.e[i] = from_float<T>(v[i]);
-  *reinterpret_cast<Raw*>(p) = raw;
+    for (int i = 0; i < N; i += 4) store_raw(p + i, u32x4{__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])});
+  } else if constexpr (N % 8 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+      store_raw(p + i, u32x4{narrow<T>(v[i], v[i + 1]), narrow<T>(v[i + 2], v[i + 3]), narrow<T>(v[i + 4], v[i + 5]), narrow<T>(v[i + 6], v[i + 7])});
+  } else {
+    store_raw(p, u32x2{narrow<T>(v[0], v[1]), narrow<T>(v[2], v[3])});
+  }
 }
 
 // The same where only the first n of the N elements exist (the others read as zero, and are not written).

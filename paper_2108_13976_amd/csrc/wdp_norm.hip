@@ -49,9 +49,50 @@ template <int TPR> __device__ __forceinline__ float row_sum(float v, float (*pla
   return total;
 }
 
-template <typename W> __device__ __forceinline__ void load_weight(const void* weight, int col, int n, float w[kVec]) {
+// Where a lane's chunk lies.  The chunk that the row ends in is moved back to end with it (rows of eight elements and
+// more): one access like the others, its first `skip` elements are its neighbour's.  (Elements one by one would cost every
+// wave of an odd width a second pass of loads: 33333 x 999 bfloat16 took 97 us forward and 172 backward that way.)
+struct Span {
+  int start, skip, count;  // count: elements that exist; 0: none
+};
+template <int TPR> __device__ __forceinline__ Span span_of(int width, int c) {
+  const int col = (c * TPR + int(threadIdx.x % TPR)) * kVec, left = width - col;
+  if (left >= kVec) return {col, 0, kVec};
+  if (left <= 0) return {0, kVec, 0};
+  return width >= kVec ? Span{width - kVec, kVec - left, kVec} : Span{0, 0, left};
+}
+// A chunk as it lies in memory: requested one row ahead of its use, where the registers hold a row more (1024 threads have
+// 128 each).
+template <int TPR, int C> constexpr bool kAhead = TPR < 1024 || C == 1;
+template <typename T> struct Words {
+  u32x4 w[sizeof(T) / 2];
+};
+template <typename T> __device__ __forceinline__ Words<T> request(const T* row, const Span& s) {
+  Words<T> r;
+  if (s.count == kVec) {
+#pragma unroll
+    for (int i = 0; i < int(sizeof(T) / 2); ++i) r.w[i] = load_raw<u32x4>(row + s.start + i * (16 / sizeof(T)));
+  } else {  // (a row of fewer than eight elements)
+    float v[kVec];
+    load_some<T, kVec>(row + s.start, s.count, v);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      if constexpr (sizeof(T) == 4) r.w[i / 4][i % 4] = __float_as_uint(v[i]);
+      else if (i % 2 == 0) r.w[0][i / 2] = narrow<T>(v[i], v[i + 1]);
+    }
+  }
+  return r;
+}
+template <typename T> __device__ __forceinline__ void values(const Words<T>& r, float v[kVec]) {
+#pragma unroll
+  for (int i = 0; i < kVec; i += sizeof(T) == 4 ? 1 : 2) {
+    if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(r.w[i / 4][i % 4]);
+    else widen<T>(r.w[0][i / 2], v + i);
+  }
+}
+template <typename W> __device__ __forceinline__ void load_weight(const void* weight, const Span& s, float w[kVec]) {
   if (weight) {
-    load_some<W, kVec>(static_cast<const W*>(weight) + col, n, w);
+    load_some<W, kVec>(static_cast<const W*>(weight) + s.start, s.count, w);
   } else {
 #pragma unroll
     for (int i = 0; i < kVec; ++i) w[i] = 1.0f;
@@ -65,68 +106,88 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
   const int lane = threadIdx.x % TPR;
   int turn = 0;
   float w[C][kVec];
-  int count[C];
+  Span at[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int col = (c * TPR + lane) * kVec;
-    count[c] = a.width - col;
-    if (C <= 2 && count[c] > 0) load_weight<W>(a.weight, col, count[c], w[c]);
+    at[c] = span_of<TPR>(a.width, c);
+    if (C <= 2 && at[c].count) load_weight<W>(a.weight, at[c], w[c]);
   }
-  for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / TPR; row < a.rows; row += int64_t(gridDim.x) * kRows) {
+  // A workgroup takes runs of 32 neighbouring rows (a whole line of scales and of rstd, four bytes a row) in turn with the
+  // others, which together go through memory from front to back: runs of a thousand rows each took 509 us for
+  // 2000000 x 256 without residual, single rounds of eight 940 with residual and scales, where runs of 32 take 428 and 767.
+  constexpr int kRun = kRows < 32 && TPR <= 64 ? 32 : kRows;
+  const auto following = [&](int64_t row) {
+    const int64_t next = row + kRows;
+    return kRun == kRows || next / kRun != row / kRun ? next + int64_t(gridDim.x - 1) * kRun : next;
+  };
+  const T *x = static_cast<const T*>(a.x), *residual = static_cast<const T*>(a.residual);
+  Words<T> next_x[C], next_r[C];
+  const auto ahead = [&](int64_t row) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if (!at[c].count) continue;
+      next_x[c] = request(x + row * a.x_stride, at[c]);
+      if (residual) next_r[c] = request(residual + row * a.residual_stride, at[c]);
+    }
+  };
+  int64_t row = int64_t(blockIdx.x) * kRun + threadIdx.x / TPR;
+  if (kAhead<TPR, C> && row < a.rows) ahead(row);
+  for (int64_t next; row < a.rows; row = next) {
+    next = following(row);
+    if (!kAhead<TPR, C>) ahead(row);
     float v[C][kVec];
     float square = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = (c * TPR + lane) * kVec;
-      if (count[c] <= 0) {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) v[c][i] = 0.0f;
-        continue;
-      }
-      load_some<T, kVec>(static_cast<const T*>(a.x) + row * a.x_stride + col, count[c], v[c]);
-      if (a.residual) {
+      for (int i = 0; i < kVec; ++i) v[c][i] = 0.0f;
+      if (!at[c].count) continue;
+      values(next_x[c], v[c]);
+      if (residual) {
         float r[kVec];
-        load_some<T, kVec>(static_cast<const T*>(a.residual) + row * a.residual_stride + col, count[c], r);
+        values(next_r[c], r);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[c][i] = to_float<T>(from_float<T>(v[c][i] + r[i]));  // the norm is that of h as it is stored
       }
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) square = fmaf(v[c][i], v[c][i], square);
+      for (int i = 0; i < kVec; ++i) square = fmaf(i < at[c].skip ? 0.0f : v[c][i], v[c][i], square);
     }
+    if (kAhead<TPR, C> && next < a.rows) ahead(next);
     const float rstd = 1.0f / sqrtf(row_sum<TPR>(square, places, turn) * a.inv_width + a.eps);
     turn ^= 1;
     if (a.rstd && lane == 0) a.rstd[row] = rstd;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = (c * TPR + lane) * kVec;
-      if (count[c] > 0 && a.h) store_some<T, kVec>(static_cast<T*>(a.h) + row * a.h_stride + col, count[c], v[c]);
-      if (C > 2 && count[c] > 0) load_weight<W>(a.weight, col, count[c], w[c]);
+      // (what a moved chunk writes of its neighbour's elements is what the neighbour writes)
+      if (at[c].count && a.h) store_some<T, kVec>(static_cast<T*>(a.h) + row * a.h_stride + at[c].start, at[c].count, v[c]);
+      if (C > 2 && at[c].count) load_weight<W>(a.weight, at[c], w[c]);
       float y[kVec];
       float most = 0.0f;
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        y[i] = i < count[c] ? v[c][i] * rstd * w[c][i] : 0.0f;
-        most = fmaxf(most, fabsf(y[i]));
+        y[i] = i < at[c].count ? v[c][i] * rstd * w[c][i] : 0.0f;
+        most = fmaxf(most, i < at[c].skip ? 0.0f : fabsf(y[i]));
       }
-      if (count[c] > 0 && a.y) store_some<T, kVec>(static_cast<T*>(a.y) + row * a.y_stride + col, count[c], y);
+      if (at[c].count && a.y) store_some<T, kVec>(static_cast<T*>(a.y) + row * a.y_stride + at[c].start, at[c].count, y);
       if (a.q) {
         most = fmaxf(group_max<(TPR < 16 ? TPR : 16)>(most), kTiny);
         const float largest = a.q_type == WDP_E4M3 ? kLargestE4M3 : kLargestE5M2;
         const float scale = most / largest, inv = 1.0f / scale;
-        if (count[c] > 0) {
+        if (at[c].count) {
           const uint32_t lo = to_codes(a.q_type, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
           const uint32_t hi = to_codes(a.q_type, y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv);
-          uint8_t* q = a.q + row * a.q_stride + col;
-          if (count[c] >= kVec) {
-            struct __attribute__((packed, aligned(1))) Codes {
-              uint32_t lo, hi;
-            };
-            *reinterpret_cast<Codes*>(q) = Codes{lo, hi};
-          } else {
-#pragma unroll
-            for (int i = 0; i < kVec; ++i)
-              if (i < count[c]) q[i] = uint8_t((i < 4 ? lo >> (8 * i) : hi >> (8 * (i - 4))) & 0xFF);
+          uint8_t* q = a.q + row * a.q_stride + at[c].start;
+          if (at[c].count == kVec && at[c].skip == 0) {
+            store_raw(q, u32x2{lo, hi});
+          } else {  // the row's end: up to seven codes, in fours, twos and ones (the neighbour's block has another scale)
+            uint64_t codes = (uint64_t(hi) << 32 | lo) >> (8 * at[c].skip);
+            q += at[c].skip;
+            const int n = at[c].count - at[c].skip;
+            if (n & 4) store_raw(q, uint32_t(codes)), codes >>= 32, q += 4;
+            if (n & 2) store_raw(q, uint16_t(codes)), codes >>= 16, q += 2;
+            if (n & 1) *q = uint8_t(codes);
           }
+          const int col = at[c].start + at[c].skip;
           if (col % WDP_BLOCK == 0) a.scale[row * a.scale_row + (col / WDP_BLOCK) * a.scale_block] = scale;
         }
       }
@@ -138,38 +199,57 @@ template <typename T, typename W, int TPR, int C>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_grad_kernel(GradArgs a) {
   constexpr int kThreads = TPR > 256 ? TPR : 256, kRows = kThreads / TPR;
   __shared__ float places[2][16];
-  const int lane = threadIdx.x % TPR;
   int turn = 0;
   float w[C][kVec], dw[C][kVec];
-  int count[C];
+  Span at[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int col = (c * TPR + lane) * kVec;
-    count[c] = a.width - col;
+    at[c] = span_of<TPR>(a.width, c);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) w[c][i] = dw[c][i] = 0.0f;
-    if (count[c] > 0) load_weight<W>(a.weight, col, count[c], w[c]);
+    if (at[c].count) load_weight<W>(a.weight, at[c], w[c]);
   }
-  for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / TPR; row < a.rows; row += int64_t(gridDim.x) * kRows) {
-    float dy[C][kVec], xhat[C][kVec];
-    float dot = 0.0f;
-    const float rstd = a.rstd[row];
+  const T *from_dy = static_cast<const T*>(a.dy), *from_h = static_cast<const T*>(a.h), *from_dh = static_cast<const T*>(a.dh);
+  Words<T> next_dy[C], next_h[C], next_dh[C];
+  float next_rstd = 0.0f;
+  const auto ahead = [&](int64_t row) {
+    next_rstd = a.rstd[row];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = (c * TPR + lane) * kVec;
-      if (count[c] <= 0) {
+      if (!at[c].count) continue;
+      next_dy[c] = request(from_dy + row * a.dy_stride, at[c]);
+      next_h[c] = request(from_h + row * a.h_stride, at[c]);
+      if (kAhead<TPR, C> && from_dh) next_dh[c] = request(from_dh + row * a.dh_stride, at[c]);
+    }
+  };
+  const int64_t step = int64_t(gridDim.x) * kRows;
+  int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / TPR;
+  if (kAhead<TPR, C> && row < a.rows) ahead(row);
+  for (; row < a.rows; row += step) {
+    if (!kAhead<TPR, C>) ahead(row);
+    float dy[C][kVec], xhat[C][kVec];
+    Words<T> dh[C];
+    float dot = 0.0f;
+    const float rstd = next_rstd;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) dy[c][i] = xhat[c][i] = 0.0f;
-        continue;
-      }
-      load_some<T, kVec>(static_cast<const T*>(a.dy) + row * a.dy_stride + col, count[c], dy[c]);
-      load_some<T, kVec>(static_cast<const T*>(a.h) + row * a.h_stride + col, count[c], xhat[c]);
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) dy[c][i] = xhat[c][i] = 0.0f;
+      if (!at[c].count) continue;
+      values(next_dy[c], dy[c]);
+      values(next_h[c], xhat[c]);
+      if (kAhead<TPR, C> && from_dh) dh[c] = next_dh[c];
+    }
+    if (kAhead<TPR, C> && row + step < a.rows) ahead(row + step);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         xhat[c][i] *= rstd;
-        dw[c][i] = fmaf(dy[c][i], xhat[c][i], dw[c][i]);
+        const float g = i < at[c].skip ? 0.0f : dy[c][i];
+        dw[c][i] = fmaf(g, xhat[c][i], dw[c][i]);
+        dot = fmaf(g * w[c][i], xhat[c][i], dot);
         dy[c][i] *= w[c][i];
-        dot = fmaf(dy[c][i], xhat[c][i], dot);
       }
     }
     if (!a.dx) continue;
@@ -177,44 +257,40 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_grad_kernel(GradAr
     turn ^= 1;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = (c * TPR + lane) * kVec;
-      if (count[c] <= 0) continue;
-      float dx[kVec];
+      if (!at[c].count) continue;
+      float dx[kVec], more[kVec];
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) dx[i] = rstd * (dy[c][i] - xhat[c][i] * mean);
-      if (a.dh) {
-        float dh[kVec];
-        load_some<T, kVec>(static_cast<const T*>(a.dh) + row * a.dh_stride + col, count[c], dh);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) dx[i] += dh[i];
+      for (int i = 0; i < kVec; ++i) more[i] = 0.0f;
+      if (from_dh) {
+        if (!kAhead<TPR, C>) dh[c] = request(from_dh + row * a.dh_stride, at[c]);
+        values(dh[c], more);
       }
-      store_some<T, kVec>(static_cast<T*>(a.dx) + row * a.dx_stride + col, count[c], dx);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) dx[i] = rstd * (dy[c][i] - xhat[c][i] * mean) + more[i];
+      store_some<T, kVec>(static_cast<T*>(a.dx) + row * a.dx_stride + at[c].start, at[c].count, dx);
     }
   }
   if (!a.partial) return;
-  // the workgroup's rows joined: every group of lanes adds its sums in LDS in turn
-  if (kRows > 1) {
-    __shared__ float joined[kRows > 1 ? kThreads * kVec : 1];
-    // [group][chunk][lane][kVec] would be C times as much: chunk by chunk instead
+  // the workgroup's rows joined in LDS, chunk by chunk, in the order of its groups of lanes
+  __shared__ float joined[kRows > 1 ? kThreads * kVec : 1];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
+  for (int c = 0; c < C; ++c) {
+    if (kRows > 1) {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < kVec; ++i) joined[threadIdx.x * kVec + i] = dw[c][i];
       __syncthreads();
-      for (int e = threadIdx.x; e < TPR * kVec; e += kThreads) {
-        const int col = c * TPR * kVec + e;
-        if (col < a.width) {
-          float sum = 0.0f;
-          for (int g = 0; g < kRows; ++g) sum += joined[g * TPR * kVec + e];
-          a.partial[int64_t(blockIdx.x) * a.width + col] = sum;
-        }
+      if (threadIdx.x < TPR) {
+        for (int g = 1; g < kRows; ++g)
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) dw[c][i] += joined[(g * TPR + threadIdx.x) * kVec + i];
       }
     }
-  } else {
+    if (threadIdx.x < TPR && at[c].count) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (count[c] > 0) store_some<float, kVec>(a.partial + int64_t(blockIdx.x) * a.width + (c * TPR + lane) * kVec, count[c], dw[c]);
+      for (int i = 0; i < kVec; ++i)
+        if (i >= at[c].skip && i < at[c].count) a.partial[int64_t(blockIdx.x) * a.width + at[c].start + i] = dw[c][i];
+    }
   }
 }
 
@@ -236,14 +312,14 @@ __global__ __launch_bounds__(1024) void norm_grad_join_kernel(const float* __res
 int rows_a_block(int width) { return width <= 32 ? 64 : width <= 64 ? 32 : width <= 128 ? 16 : width <= 256 ? 8 : width <= 1024 ? 4 : 1; }
 
 int64_t grad_blocks(const wdp_norm_config& c) {
-  const int64_t per = rows_a_block(c.width), all = (c.rows + per - 1) / per, most = c.width > 4096 ? 256 : 512;
+  const int64_t per = rows_a_block(c.width), all = (c.rows + per - 1) / per, most = c.width > 4096 ? 256 : 1024;
   return all < most ? all : most;
 }
 
 template <typename T, typename W> struct Norm {
   template <int TPR, int C> static void run(const NormArgs& a, hipStream_t stream) {
-    constexpr int threads = TPR > 256 ? TPR : 256, per = threads / TPR;
-    const int64_t all = (a.rows + per - 1) / per, most = 2048 * 256 / threads;
+    constexpr int threads = TPR > 256 ? TPR : 256, per = threads / TPR, run = per < 32 && TPR <= 64 ? 32 : per;
+    const int64_t all = (a.rows + run - 1) / run, most = 2048 * 256 / threads;
     norm_kernel<T, W, TPR, C><<<dim3(unsigned(all < most ? all : most)), dim3(threads), 0, stream>>>(a);
   }
 };

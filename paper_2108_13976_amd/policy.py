@@ -109,42 +109,85 @@ def wdp_adamw(cfg, tensors, count):
 
 
 # ---- tensors ------------------------------------------------------------------------------------
-_FLOATS = _EIGHTS = None
+_FLOATS = _EIGHTS = _F32 = _module = None
+
+
+def _torch():
+    """torch, looked up late: the ABI part of this module works without tensors."""
+    global _module
+    if _module is None:
+        import torch
+
+        _module = torch
+    return _module
 
 
 def _types():
-    """torch's names of the element types (looked up late: the ABI part of this module works without tensors)."""
-    global _FLOATS, _EIGHTS
+    """torch's names of the element types."""
+    global _FLOATS, _EIGHTS, _F32
     if _FLOATS is None:
-        import torch
-
-        _FLOATS = {torch.float32: WDP_F32, torch.bfloat16: WDP_BF16, torch.float16: WDP_F16}
+        torch = _torch()
+        _F32 = torch.float32
         _EIGHTS = {torch.float8_e4m3fn: WDP_E4M3, torch.float8_e5m2: WDP_E5M2}
+        _FLOATS = {torch.float32: WDP_F32, torch.bfloat16: WDP_BF16, torch.float16: WDP_F16}
     return _FLOATS, _EIGHTS
 
 
-class _on:
-    """The tensors' device as the current one, and its current stream; raises without a GPU."""
+_stream_of = _current = None  # raw handle of a device's current stream; number of the current device
 
-    __slots__ = ("stream", "guard")
 
-    def __init__(self, what, tensor):
-        import torch
+def _late():
+    global _stream_of, _current
+    torch = _torch()
+    _types()
+    _library()
+    torch.cuda.init()
+    _stream_of, _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
-        device = tensor.device
-        if device.type != "cuda":
-            raise RuntimeError(f"{what} needs tensors on a GPU: the HIP path has no CPU fallback")
-        self.stream = torch.cuda.current_stream(device).cuda_stream
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream
+# What a call's checks and its config come to depends on its tensors' types, shapes, strides and device, not on what is in
+# them or where they lie: it is worked out once for each such set (and stream), which saves a small call half its time on the host.
+_plans = {}
+_MOST_PLANS = 1024
 
-    def __exit__(self, *error):
-        if self.guard is not None:
-            self.guard.__exit__(*error)
+
+def _key(what, device, *parts):
+    """The key of a call's plan, or a refusal of tensors on the CPU."""
+    if device < 0:
+        raise RuntimeError(f"{what} needs tensors on a GPU: the HIP path has no CPU fallback")
+    if _stream_of is None:
+        _late()
+    return (what, device, _stream_of(device), parts)
+
+
+def _gpu(what, key):
+    """The stream of a key, once the arguments have been found right; refuses tensors on the CPU."""
+    if key is None:
+        _key(what, -1)
+    return key[2]
+
+
+def _keep(key, plan):
+    if len(_plans) >= _MOST_PLANS:
+        _plans.clear()
+    _plans[key] = plan
+    return plan
+
+
+def _of(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
+
+
+def _call(device, name, cfg, bufs):
+    """An entry point of the library, on its device."""
+    call = getattr(_declared or _library(), name)
+    if _current() == device:
+        rc = call(cfg, bufs)
+    else:
+        with _torch().cuda.device(device):
+            rc = call(cfg, bufs)
+    if rc != WD_OK:
+        raise WdError(rc, name)
 
 
 def _check(what, name, tensor, like, dtypes, shape=None):
@@ -152,8 +195,15 @@ def _check(what, name, tensor, like, dtypes, shape=None):
         raise ValueError(f"{what}: {name} is on {tensor.device}, not on {like.device}")
     if tensor.dtype not in dtypes:
         raise ValueError(f"{what}: {name} has type {tensor.dtype}")
-    if shape is not None and tuple(tensor.shape) != tuple(shape):
+    if shape is not None and tensor.shape != shape:
         raise ValueError(f"{what}: {name} has shape {tuple(tensor.shape)}, not {tuple(shape)}")
+
+
+def _check_weight(what, weight, like, width):
+    if weight is not None:
+        _check(what, "weight", weight, like, (_F32, like.dtype), (width,))
+        if not weight.is_contiguous():
+            raise ValueError(f"{what}: weight is not contiguous")
 
 
 def _rows(what, name, tensor):
@@ -190,8 +240,27 @@ def rms_norm(x, weight=None, residual=None, eps=1e-5, out8=None, y=None, h=None)
     rstd: [rows] float32, what ``rms_norm_backward`` needs beside h.  x may be float32, bfloat16 or float16; weight
     float32 or x's type, None for ones.
     """
-    import torch
+    device = x.get_device()
+    key = _key("rms_norm", device, _of(x), _of(weight), _of(residual), _of(h), eps, out8, y) if device >= 0 else None
+    plan = _plans.get(key) or _plan_norm(key, x, weight, residual, eps, out8, y, h)
+    cfg, rows, want_y, q_shape, scale_shape, cut = plan
+    empty = _torch().empty
+    if residual is not None and h is None:
+        h = empty(x.shape, dtype=x.dtype, device=x.device)
+    rstd = empty(rows, dtype=_F32, device=x.device)
+    out = empty(x.shape, dtype=x.dtype, device=x.device) if want_y else None
+    q = scale = None
+    if out8 is not None:
+        q = empty(q_shape, dtype=out8, device=x.device)
+        scale = empty(scale_shape, dtype=_F32, device=x.device).t()
+    _call(device, "wdp_norm", cfg, wdp_norm_buffers(
+        x.data_ptr(), None if residual is None else residual.data_ptr(), None if weight is None else weight.data_ptr(),
+        None if h is None else h.data_ptr(), out.data_ptr() if want_y else None, None if q is None else q.data_ptr(),
+        None if q is None else scale.data_ptr(), rstd.data_ptr()))
+    return NormOut(x if h is None else h, out, q if cut is None else q[:, :cut], scale, rstd)
 
+
+def _plan_norm(key, x, weight, residual, eps, out8, y, h):
     floats, eights = _types()
     what = "rms_norm"
     if x.dtype not in floats:
@@ -199,50 +268,49 @@ def rms_norm(x, weight=None, residual=None, eps=1e-5, out8=None, y=None, h=None)
     rows, width, x_stride = _rows(what, "x", x)
     if not width:
         raise ValueError(f"{what}: x has no elements in a row")
-    if weight is not None:
-        _check(what, "weight", weight, x, (torch.float32, x.dtype), (width,))
-        if not weight.is_contiguous():
-            raise ValueError(f"{what}: weight is not contiguous")
+    _check_weight(what, weight, x, width)
     if out8 is not None and out8 not in eights:
         raise ValueError(f"{what}: out8 is {out8}")
     want_y = out8 is None if y is None else bool(y)
     if not want_y and out8 is None:
         raise ValueError(f"{what}: nothing to compute")
-    residual_stride = h_stride = 0
+    residual_stride = h_stride = width
     if residual is not None:
         _check(what, "residual", residual, x, (x.dtype,), x.shape)
         residual_stride = _rows(what, "residual", residual)[2]
-        if h is None:
-            h = torch.empty_like(x, memory_format=torch.contiguous_format)
-        else:
+        if h is not None:
             _check(what, "h", h, x, (x.dtype,), x.shape)
-        h_stride = _rows(what, "h", h)[2]
+            h_stride = _rows(what, "h", h)[2]
     elif h is not None:
         raise ValueError(f"{what}: h without a residual")
-    with _on(what, x) as stream:
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_y else None
-        q = scale = None
-        q_stride = -(-width // 16) * 16
-        if out8 is not None:
-            q = torch.empty((rows, q_stride), dtype=out8, device=x.device)
-            # the scales of a block lie side by side: the product reads them row by row of its tiles
-            scale = torch.empty((-(-width // WDP_BLOCK), rows), dtype=torch.float32, device=x.device).t()
-        cfg = wdp_norm_config(ctypes.sizeof(wdp_norm_config), floats[x.dtype], WDP_F32 if weight is None else floats[weight.dtype],
-                              eights[out8] if out8 is not None else 0, rows, width, eps, x_stride, residual_stride, h_stride, width, q_stride,
-                              1, rows, 0, 0, 0, stream)
-        wdp_norm(cfg, wdp_norm_buffers(
-            x.data_ptr(), residual.data_ptr() if residual is not None else None, weight.data_ptr() if weight is not None else None,
-            h.data_ptr() if residual is not None else None, out.data_ptr() if want_y else None, q.data_ptr() if q is not None else None,
-            scale.data_ptr() if q is not None else None, rstd.data_ptr()))
-    return NormOut(x if residual is None else h, out, None if q is None else q[:, :width] if q_stride != width else q, scale, rstd)
+    q_stride, blocks = -(-width // 16) * 16, -(-width // WDP_BLOCK)
+    # (the scales of a block lie side by side: the product reads them row by row of its tiles)
+    cfg = wdp_norm_config(ctypes.sizeof(wdp_norm_config), floats[x.dtype], WDP_F32 if weight is None else floats[weight.dtype],
+                          eights[out8] if out8 is not None else 0, rows, width, eps, x_stride, residual_stride, h_stride, width, q_stride,
+                          1, rows, 0, 0, 0, _gpu(what, key))
+    return _keep(key, (cfg, rows, want_y, (rows, q_stride), (blocks, rows), width if out8 is not None and q_stride != width else None))
 
 
 def rms_norm_backward(dy, h, weight, rstd, dh=None, want_dw=True):
     """(dx, dw) of ``rms_norm`` from the gradients of y and (``dh``, may be None) of h: dx is the gradient of x and of
     residual alike, in h's type; dw [D] float32, None with ``want_dw=False``.  weight None: ones."""
-    import torch
+    device = h.get_device()
+    key = _key("rms_norm_backward", device, _of(dy), _of(h), _of(weight), _of(rstd), _of(dh)) if device >= 0 else None
+    plan = _plans.get(key) or _plan_norm_backward(key, dy, h, weight, rstd, dh)
+    cfg, width, need = plan
+    empty = _torch().empty
+    dx = empty(h.shape, dtype=h.dtype, device=h.device)
+    dw = space = None
+    if want_dw:
+        dw = empty(width, dtype=_F32, device=h.device)
+        space = empty(need, dtype=_torch().uint8, device=h.device)
+    _call(device, "wdp_norm_backward", cfg, wdp_norm_grad_buffers(
+        dy.data_ptr(), None if dh is None else dh.data_ptr(), h.data_ptr(), None if weight is None else weight.data_ptr(),
+        rstd.data_ptr(), dx.data_ptr(), dw.data_ptr() if want_dw else None, space.data_ptr() if want_dw else None))
+    return dx, dw
 
+
+def _plan_norm_backward(key, dy, h, weight, rstd, dh):
     floats, _ = _types()
     what = "rms_norm_backward"
     if h.dtype not in floats:
@@ -251,29 +319,17 @@ def rms_norm_backward(dy, h, weight, rstd, dh=None, want_dw=True):
     if not width:
         raise ValueError(f"{what}: h has no elements in a row")
     _check(what, "dy", dy, h, (h.dtype,), h.shape)
-    _check(what, "rstd", rstd, h, (torch.float32,), (rows,))
+    _check(what, "rstd", rstd, h, (_F32,), (rows,))
     if not rstd.is_contiguous():
         raise ValueError(f"{what}: rstd is not contiguous")
-    if weight is not None:
-        _check(what, "weight", weight, h, (torch.float32, h.dtype), (width,))
-        if not weight.is_contiguous():
-            raise ValueError(f"{what}: weight is not contiguous")
-    dh_stride = 0
+    _check_weight(what, weight, h, width)
+    dh_stride = width
     if dh is not None:
         _check(what, "dh", dh, h, (h.dtype,), h.shape)
         dh_stride = _rows(what, "dh", dh)[2]
-    with _on(what, h) as stream:
-        dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-        cfg = wdp_norm_config(ctypes.sizeof(wdp_norm_config), floats[h.dtype], WDP_F32 if weight is None else floats[weight.dtype], 0, rows, width,
-                              0.0, 0, 0, h_stride, 0, 0, 0, 0, _rows(what, "dy", dy)[2], dh_stride, width, stream)
-        dw = space = None
-        if want_dw:
-            dw = torch.empty(width, dtype=torch.float32, device=h.device)
-            space = torch.empty(wdp_norm_backward_workspace(cfg), dtype=torch.uint8, device=h.device)
-        wdp_norm_backward(cfg, wdp_norm_grad_buffers(
-            dy.data_ptr(), dh.data_ptr() if dh is not None else None, h.data_ptr(), weight.data_ptr() if weight is not None else None,
-            rstd.data_ptr(), dx.data_ptr(), dw.data_ptr() if want_dw else None, space.data_ptr() if want_dw else None))
-    return dx, dw
+    cfg = wdp_norm_config(ctypes.sizeof(wdp_norm_config), floats[h.dtype], WDP_F32 if weight is None else floats[weight.dtype], 0, rows, width,
+                          0.0, width, width, h_stride, width, width, 0, 0, _rows(what, "dy", dy)[2], dh_stride, width, _gpu(what, key))
+    return _keep(key, (cfg, width, wdp_norm_backward_workspace(cfg)))
 
 
 def quantise8(w, dtype=None, rows=128):
@@ -300,37 +356,44 @@ def product8(a, a_scale, b, b_scale, dtype=None, out=None):
     """``a`` [m, k] times the transpose of ``b`` [n, k], both 8-bit with scales for blocks of 128 along k: [m, n] in
     ``dtype`` (bfloat16; float32, float16) or into ``out``.  a_scale [m, blocks]; b_scale [ceil(n / 128), blocks], or
     [n, blocks] for a scale per row; both float32, of any strides.  Rows that start at 16-byte boundaries run faster."""
-    import torch
+    device = a.get_device()
+    key = _key("product8", device, _of(a), _of(a_scale), _of(b), _of(b_scale), dtype, _of(out)) if device >= 0 else None
+    plan = _plans.get(key) or _plan_product(key, a, a_scale, b, b_scale, dtype, out)
+    cfg, shape, out_dtype, need = plan
+    empty = _torch().empty
+    if out is None:
+        out = empty(shape, dtype=out_dtype, device=a.device)
+    space = empty(need, dtype=_torch().uint8, device=a.device) if need else None
+    _call(device, "wdp_product", cfg, wdp_product_buffers(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), out.data_ptr(),
+                                                          space.data_ptr() if need else None))
+    return out
 
+
+def _plan_product(key, a, a_scale, b, b_scale, dtype, out):
     floats, eights = _types()
     what = "product8"
     if a.dim() != 2 or b.dim() != 2 or a.dtype not in eights:
         raise ValueError(f"{what}: a is an 8-bit matrix, b another")
-    (m, k, a_stride), (n, kb, b_stride) = _rows(what, "a", a), _rows(what, "b", b)
+    (m, k, a_stride), (n, _, b_stride) = _rows(what, "a", a), _rows(what, "b", b)
     _check(what, "b", b, a, tuple(eights), (n, k))
     if not k:
         raise ValueError(f"{what}: a has no elements in a row")
     blocks, groups = -(-k // WDP_BLOCK), -(-n // WDP_BLOCK)
-    _check(what, "a_scale", a_scale, a, (torch.float32,), (m, blocks))
-    by_row = b_scale.shape[0] == n and n != groups
-    _check(what, "b_scale", b_scale, a, (torch.float32,), (n if by_row else groups, blocks))
+    _check(what, "a_scale", a_scale, a, (_F32,), (m, blocks))
+    by_row = b_scale.dim() == 2 and b_scale.shape[0] == n and n != groups
+    _check(what, "b_scale", b_scale, a, (_F32,), (n if by_row else groups, blocks))
     if out is None:
-        dtype = torch.bfloat16 if dtype is None else dtype
+        dtype = _torch().bfloat16 if dtype is None else dtype
         if dtype not in floats:
             raise ValueError(f"{what}: dtype is {dtype}")
         c_stride = n
     else:
         _check(what, "out", out, a, tuple(floats) if dtype is None else (dtype,), (m, n))
         c_stride = _rows(what, "out", out)[2]
-    with _on(what, a) as stream:
-        if out is None:
-            out = torch.empty((m, n), dtype=dtype, device=a.device)
-        cfg = wdp_product_config(ctypes.sizeof(wdp_product_config), eights[a.dtype], eights[b.dtype], floats[out.dtype], m, n, k,
-                                 1 if by_row else WDP_BLOCK, a_stride, b_stride, c_stride, *a_scale.stride(), *b_scale.stride(), stream)
-        need = wdp_product_workspace(cfg)
-        space = torch.empty(need, dtype=torch.uint8, device=a.device).data_ptr() if need else None
-        wdp_product(cfg, wdp_product_buffers(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), out.data_ptr(), space))
-    return out
+        dtype = out.dtype
+    cfg = wdp_product_config(ctypes.sizeof(wdp_product_config), eights[a.dtype], eights[b.dtype], floats[dtype], m, n, k,
+                             1 if by_row else WDP_BLOCK, a_stride, b_stride, c_stride, *a_scale.stride(), *b_scale.stride(), _gpu(what, key))
+    return _keep(key, (cfg, (m, n), dtype, wdp_product_workspace(cfg)))
 
 
 def verify_drafts(target, draft_probs, drafts, u, lengths=None, tokens=None):
@@ -339,10 +402,26 @@ def verify_drafts(target, draft_probs, drafts, u, lengths=None, tokens=None):
     uniform numbers, n for the drafts and one for the draw; they must not be those that drew the drafts.  lengths [B]
     int32: how many of a sequence's drafts count.  accepted [B] int32; tokens [B, rows of target] int32: the accepted
     drafts, the drawn token, -1.  tokens: where to write them (``drafts`` itself where target has n rows)."""
-    import torch
+    device = target.get_device()
+    key = _key("verify_drafts", device, _of(target), _of(draft_probs), _of(drafts), _of(u), _of(lengths), _of(tokens)) if device >= 0 else None
+    plan = _plans.get(key) or _plan_verify(key, target, draft_probs, drafts, u, lengths, tokens)
+    cfg, batch, rows, n, need = plan
+    empty, i32 = _torch().empty, _torch().int32
+    accepted = empty(batch, dtype=i32, device=target.device)
+    if tokens is None:
+        tokens = empty((batch, rows), dtype=i32, device=target.device)
+    elif rows > n and n and tokens.data_ptr() == drafts.data_ptr():
+        raise ValueError("verify_drafts: tokens can be drafts only where target has a row for each draft")
+    space = empty(need, dtype=_torch().uint8, device=target.device) if need else None
+    _call(device, "wdp_verify", cfg, wdp_verify_buffers(
+        target.data_ptr(), draft_probs.data_ptr() if n else None, drafts.data_ptr() if n else None,
+        None if lengths is None else lengths.data_ptr(), u.data_ptr(), accepted.data_ptr(), tokens.data_ptr(), space.data_ptr() if need else None))
+    return accepted, tokens
 
+
+def _plan_verify(key, target, draft_probs, drafts, u, lengths, tokens):
     floats, _ = _types()
-    what = "verify_drafts"
+    what, i32 = "verify_drafts", _torch().int32
     if target.dim() != 3 or draft_probs.dim() != 3 or target.dtype not in floats:
         raise ValueError(f"{what}: target and draft_probs are [B, rows, V]")
     batch, rows, vocab = target.shape
@@ -350,33 +429,21 @@ def verify_drafts(target, draft_probs, drafts, u, lengths=None, tokens=None):
     if not vocab or rows - n not in (0, 1) or rows < 1:
         raise ValueError(f"{what}: target has {rows} rows for {n} drafts")
     _check(what, "draft_probs", draft_probs, target, (target.dtype,), (batch, n, vocab))
-    _check(what, "drafts", drafts, target, (torch.int32,), (batch, n))
-    _check(what, "u", u, target, (torch.float32,), (batch, n + 1))
+    _check(what, "drafts", drafts, target, (i32,), (batch, n))
+    _check(what, "u", u, target, (_F32,), (batch, n + 1))
     for name, t in (("target", target), ("draft_probs", draft_probs)):
         if vocab > 1 and t.numel() and t.stride(2) != 1:
             raise ValueError(f"{what}: a row's elements have to be adjacent in {name}")
-    if not (drafts.is_contiguous() and u.is_contiguous()):
-        raise ValueError(f"{what}: drafts and u have to be contiguous")
-    if lengths is not None:
-        _check(what, "lengths", lengths, target, (torch.int32,), (batch,))
-        if not lengths.is_contiguous():
-            raise ValueError(f"{what}: lengths is not contiguous")
-    if tokens is not None:
-        _check(what, "tokens", tokens, target, (torch.int32,), (batch, rows))
-        if not tokens.is_contiguous():
-            raise ValueError(f"{what}: tokens is not contiguous")
-    with _on(what, target) as stream:
-        accepted = torch.empty(batch, dtype=torch.int32, device=target.device)
-        if tokens is None:
-            tokens = torch.empty((batch, rows), dtype=torch.int32, device=target.device)
-        (tb, tr, _), (db, dr, _) = target.stride(), draft_probs.stride()
-        cfg = wdp_verify_config(ctypes.sizeof(wdp_verify_config), floats[target.dtype], batch, n, vocab, rows - n, tb, tr, db, dr, stream)
-        need = wdp_verify_workspace(cfg)
-        space = torch.empty(need, dtype=torch.uint8, device=target.device).data_ptr() if need else None
-        wdp_verify(cfg, wdp_verify_buffers(target.data_ptr(), draft_probs.data_ptr() if n else None, drafts.data_ptr() if n else None,
-                                           lengths.data_ptr() if lengths is not None else None, u.data_ptr(), accepted.data_ptr(),
-                                           tokens.data_ptr(), space))
-    return accepted, tokens
+    for name, t, shape in (("drafts", drafts, None), ("u", u, None), ("lengths", lengths, (batch,)), ("tokens", tokens, (batch, rows))):
+        if t is None:
+            continue
+        if shape is not None:
+            _check(what, name, t, target, (i32,), shape)
+        if not t.is_contiguous():
+            raise ValueError(f"{what}: {name} is not contiguous")
+    (tb, tr, _), (db, dr, _) = target.stride(), draft_probs.stride()
+    cfg = wdp_verify_config(ctypes.sizeof(wdp_verify_config), floats[target.dtype], batch, n, vocab, rows - n, tb, tr, db, dr, _gpu(what, key))
+    return _keep(key, (cfg, batch, rows, n, wdp_verify_workspace(cfg)))
 
 
 class AdamW:
@@ -446,21 +513,22 @@ class AdamW:
         """One update.  step: its number (one more than the last by default).  step_device: an int64 device tensor that
         holds the number when the kernel runs, for steps captured into a HIP graph.  grad_scale: a float32 device tensor
         that the gradients are multiplied by (a clipping factor)."""
-        import torch
-
         what = "AdamW.step"
         first = self.params[0]
-        if step_device is not None:
-            _check(what, "step_device", step_device, first, (torch.int64,))
-        if grad_scale is not None:
-            _check(what, "grad_scale", grad_scale, first, (torch.float32,))
-        for t in (step_device, grad_scale):
-            if t is not None and t.numel() != 1:
-                raise ValueError(f"{what}: one number on the device, not {t.numel()}")
+        for name, t, dtype in (("step_device", step_device, _torch().int64), ("grad_scale", grad_scale, _F32)):
+            if t is not None:
+                _check(what, name, t, first, (dtype,))
+                if t.numel() != 1:
+                    raise ValueError(f"{what}: one number on the device, not {t.numel()}")
         number = self.steps + 1 if step is None else int(step)
-        with _on(what, first) as stream:
-            wdp_adamw(wdp_adamw_config(ctypes.sizeof(wdp_adamw_config), self.state_bits, self.lr, self.betas[0], self.betas[1], self.eps,
-                                       self.weight_decay, number, step_device.data_ptr() if step_device is not None else None,
-                                       grad_scale.data_ptr() if grad_scale is not None else None, self.seed, stream),
-                      self._table, len(self.params))
+        device = first.get_device()
+        cfg = wdp_adamw_config(ctypes.sizeof(wdp_adamw_config), self.state_bits, self.lr, self.betas[0], self.betas[1], self.eps,
+                               self.weight_decay, number, None if step_device is None else step_device.data_ptr(),
+                               None if grad_scale is None else grad_scale.data_ptr(), self.seed, _key(what, device)[2])
+        table, count = self._table, len(self.params)
+        if _current() == device:
+            wdp_adamw(cfg, table, count)
+        else:
+            with _torch().cuda.device(device):
+                wdp_adamw(cfg, table, count)
         self.steps = number
