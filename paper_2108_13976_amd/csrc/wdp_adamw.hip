@@ -40,16 +40,22 @@ static_assert(sizeof(AdamArgs) <= 4096, "a launch's arguments");
 __device__ __forceinline__ void philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1, uint32_t w[4]) {
 #pragma unroll
   for (int round = 0; round < 10; ++round) {
-    const uint32_t hi_a = __umulhi(0xD2511F53u, c0), lo_a = 0xD2511F53u * c0;
-    const uint32_t hi_b = __umulhi(0xCD9E8D57u, c2), lo_b = 0xCD9E8D57u * c2;
-    c0 = hi_b ^ c1 ^ k0;
-    c1 = lo_b;
-    c2 = hi_a ^ c3 ^ k1;
-    c3 = lo_a;
+    const uint64_t x = uint64_t(0xD2511F53u) * c0, y = uint64_t(0xCD9E8D57u) * c2;  // (one instruction each)
+    c0 = uint32_t(y >> 32) ^ c1 ^ k0;
+    c1 = uint32_t(y);
+    c2 = uint32_t(x >> 32) ^ c3 ^ k1;
+    c3 = uint32_t(x);
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
   w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
+}
+
+// x / d from the rounded 1 / d: the product, put right by its remainder, is the quotient rounded once (but where it
+// underflows).  A tenth of a division's instructions count here: the 8-bit step is bound by instructions beside memory.
+__device__ __forceinline__ float quotient(float x, float d, float per) {
+  const float q = x * per;
+  return fmaf(fmaf(-q, d, x), per, q);
 }
 
 // v (its size at most 448, or NaN) to a neighbour in E4M3, by 16 random bits: in units of the code's step at v,
@@ -112,7 +118,7 @@ template <typename P, typename G, bool EIGHT> __global__ __launch_bounds__(kThre
   }
   const float gscale = a.grad_scale ? *a.grad_scale : 1.0f;
   const int n = t.numel - at >= kVec ? kVec : t.numel > at ? int(t.numel - at) : 0;
-  float p[kVec], g[kVec], m[kVec], v[kVec];
+  float p[kVec], g[kVec], m[kVec], v[kVec], root[kVec];
 #pragma unroll
   for (int i = 0; i < kVec; ++i) p[i] = g[i] = m[i] = v[i] = 0.0f;
   if (n) {
@@ -139,7 +145,8 @@ template <typename P, typename G, bool EIGHT> __global__ __launch_bounds__(kThre
     g[i] *= gscale;
     m[i] = a.b1 * m[i] + a.rest1 * g[i];
     v[i] = a.b2 * v[i] + a.rest2 * g[i] * g[i];
-    p[i] = p[i] * a.decay - c1 * m[i] / (sqrtf(v[i]) * c2 + a.eps);
+    root[i] = sqrtf(v[i]);
+    p[i] = p[i] * a.decay - c1 * m[i] / (root[i] * c2 + a.eps);
   }
   if (n) {
     if (t.master) store_some<float, kVec>(t.master + at, n, p);
@@ -153,12 +160,12 @@ template <typename P, typename G, bool EIGHT> __global__ __launch_bounds__(kThre
     float most_m = 0.0f, most_s = 0.0f;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      if (i >= n) m[i] = v[i] = 0.0f;
-      v[i] = sqrtf(v[i]);
+      if (i >= n) m[i] = root[i] = 0.0f;
       most_m = fmaxf(most_m, fabsf(m[i]));
-      most_s = fmaxf(most_s, v[i]);
+      most_s = fmaxf(most_s, root[i]);
     }
     const float ms = fmaxf(group_max<16>(most_m), kTiny) * (1.0f / kLargestE4M3), vs = fmaxf(group_max<16>(most_s), kTiny) * (1.0f / kLargestE4M3);
+    const float per_m = 1.0f / ms, per_s = 1.0f / vs;
     if (n) {
       const uint64_t block = a.number[which] + uint64_t(at / WDP_BLOCK);
       const uint64_t four = block * (WDP_BLOCK / 4) + (at % WDP_BLOCK) / 4;
@@ -168,13 +175,13 @@ template <typename P, typename G, bool EIGHT> __global__ __launch_bounds__(kThre
       philox(uint32_t(four + 1), uint32_t((four + 1) >> 32), uint32_t(step), stream, a.seed_lo, a.seed_hi, w + 4);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        const bool some = v[i] > 0.0f;
-        m[i] = round_at_random(m[i] / ms, w[i] & 0xFFFFu);
-        v[i] = round_at_random(v[i] / vs, w[i] >> 16);
-        if (some) v[i] = fmaxf(v[i], 0.001953125f);  // 2^-9, the least code: the step that follows divides by it
+        const bool some = root[i] > 0.0f;
+        m[i] = round_at_random(quotient(m[i], ms, per_m), w[i] & 0xFFFFu);
+        root[i] = round_at_random(quotient(root[i], vs, per_s), w[i] >> 16);
+        if (some) root[i] = fmaxf(root[i], 0.001953125f);  // 2^-9, the least code: the step that follows divides by it
       }
       write_codes(static_cast<uint8_t*>(t.exp_avg) + at, n, m);
-      write_codes(static_cast<uint8_t*>(t.exp_avg_sq) + at, n, v);
+      write_codes(static_cast<uint8_t*>(t.exp_avg_sq) + at, n, root);
       if (at % WDP_BLOCK == 0) {
         t.avg_scale[at / WDP_BLOCK] = ms;
         t.sq_scale[at / WDP_BLOCK] = vs;

@@ -21,6 +21,7 @@ struct NormArgs {
   float *scale, *rstd;
   int64_t rows, x_stride, residual_stride, h_stride, y_stride, q_stride, scale_row, scale_block;
   int32_t width, q_type;
+  int32_t run;  // rows that a workgroup takes one after the other: a power of two
   float eps, inv_width;
 };
 
@@ -115,10 +116,10 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
   // A workgroup takes runs of 32 neighbouring rows (a whole line of scales and of rstd, four bytes a row) in turn with the
   // others, which together go through memory from front to back: runs of a thousand rows each took 509 us for
   // 2000000 x 256 without residual, single rounds of eight 940 with residual and scales, where runs of 32 take 428 and 767.
-  constexpr int kRun = kRows < 32 && TPR <= 64 ? 32 : kRows;
+  const int run = a.run;
   const auto following = [&](int64_t row) {
     const int64_t next = row + kRows;
-    return kRun == kRows || next / kRun != row / kRun ? next + int64_t(gridDim.x - 1) * kRun : next;
+    return run == kRows || next % run < kRows ? next + int64_t(gridDim.x - 1) * run : next;
   };
   const T *x = static_cast<const T*>(a.x), *residual = static_cast<const T*>(a.residual);
   Words<T> next_x[C], next_r[C];
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
       if (residual) next_r[c] = request(residual + row * a.residual_stride, at[c]);
     }
   };
-  int64_t row = int64_t(blockIdx.x) * kRun + threadIdx.x / TPR;
+  int64_t row = int64_t(blockIdx.x) * run + threadIdx.x / TPR;
   if (kAhead<TPR, C> && row < a.rows) ahead(row);
   for (int64_t next; row < a.rows; row = next) {
     next = following(row);
@@ -294,17 +295,28 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_grad_kernel(GradAr
   }
 }
 
-// dw from the workgroups' sums: 32 columns a workgroup, 32 threads a column, in a fixed order.
+// dw from the workgroups' sums: 16 columns a workgroup, 64 threads a column, in a fixed order.
 __global__ __launch_bounds__(1024) void norm_grad_join_kernel(const float* __restrict__ partial, int parts, int width, float* __restrict__ dw) {
-  __shared__ float sums[32][33];
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, col = blockIdx.x * 32 + x;
+  __shared__ float sums[64][17];
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4, col = blockIdx.x * 16 + x;
   float sum = 0.0f;
-  if (col < width)
-    for (int p = y; p < parts; p += 32) sum += partial[int64_t(p) * width + col];
+  if (col < width) {
+#pragma unroll 4
+    for (int p = y; p < parts; p += 64) sum += partial[int64_t(p) * width + col];
+  }
   sums[y][x] = sum;
   __syncthreads();
+  if (y < 8) {
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += sums[y * 8 + i][x];
+    sums[y * 8][x] = sum;
+  }
+  __syncthreads();
   if (y == 0 && col < width) {
-    for (int i = 1; i < 32; ++i) sum += sums[i][x];
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += sums[i * 8][x];
     dw[col] = sum;
   }
 }
@@ -317,9 +329,11 @@ int64_t grad_blocks(const wdp_norm_config& c) {
 }
 
 template <typename T, typename W> struct Norm {
-  template <int TPR, int C> static void run(const NormArgs& a, hipStream_t stream) {
-    constexpr int threads = TPR > 256 ? TPR : 256, per = threads / TPR, run = per < 32 && TPR <= 64 ? 32 : per;
-    const int64_t all = (a.rows + run - 1) / run, most = 2048 * 256 / threads;
+  template <int TPR, int C> static void run(NormArgs a, hipStream_t stream) {
+    constexpr int threads = TPR > 256 ? TPR : 256, per = threads / TPR;
+    const int64_t most = 2048 * 256 / threads;
+    a.run = per < 32 && TPR <= 64 && a.rows > 32 * most ? 32 : per;  // (few rows: one round of as many workgroups as there can be)
+    const int64_t all = (a.rows + a.run - 1) / a.run;
     norm_kernel<T, W, TPR, C><<<dim3(unsigned(all < most ? all : most)), dim3(threads), 0, stream>>>(a);
   }
 };
@@ -386,7 +400,7 @@ int wdp_norm(const wdp_norm_config* cfg, const wdp_norm_buffers* b) {
     return WD_E_ALIGN;
   const NormArgs a = {b->x, b->residual, b->weight, b->h, b->y, static_cast<uint8_t*>(b->q), b->scale, b->rstd, cfg->rows, cfg->x_stride,
                       cfg->residual_stride, cfg->h_stride, cfg->y_stride, cfg->q_stride, cfg->scale_row_stride, cfg->scale_block_stride,
-                      cfg->width, cfg->q_type, cfg->eps, float(1.0 / cfg->width)};
+                      cfg->width, cfg->q_type, 0, cfg->eps, float(1.0 / cfg->width)};
   by_type<Norm>(cfg->type, cfg->weight_type, cfg->width, a, static_cast<hipStream_t>(cfg->stream));
   return launched();
 }
@@ -428,7 +442,7 @@ int wdp_norm_backward(const wdp_norm_config* cfg, const wdp_norm_grad_buffers* b
     if (status != WD_OK) return status;
   }
   if (b->dw) {  // (of no rows: zeros)
-    norm_grad_join_kernel<<<dim3(unsigned((cfg->width + 31) / 32)), dim3(1024), 0, stream>>>(static_cast<const float*>(b->workspace), int(blocks), cfg->width, b->dw);
+    norm_grad_join_kernel<<<dim3(unsigned((cfg->width + 15) / 16)), dim3(1024), 0, stream>>>(static_cast<const float*>(b->workspace), int(blocks), cfg->width, b->dw);
     return launched();
   }
   return WD_OK;

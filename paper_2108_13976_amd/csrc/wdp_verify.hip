@@ -5,24 +5,24 @@
 // floats (exact in float64) against a float; the draw compares float64 sums, whose order moves a border by 1e-16 of
 // the row's sum, so that the kernels below, which sum in different orders, answer alike.
 //
-// Three forms by the vocabulary.  Few actions (a policy of Tag has five): a lane a sequence.  Rows that a workgroup
-// holds in registers: a workgroup (or a wave) a sequence.  Longer rows: a workgroup a piece of 4096 elements sums it,
-// a second launch finds the piece that holds the drawn token and goes through that one alone.
+// Forms by the vocabulary.  Few actions (a policy of Tag has five): a lane a sequence, the row in its registers.  Up to
+// 1024: sixteen lanes or a wave a sequence, no barrier.  Up to 4096: a workgroup.  Longer rows: a workgroup a piece of 4096
+// elements sums it, a second launch finds the piece that holds the drawn token and goes through that one alone.  Memory
+// bounds the large batches, the chain of dependent loads (drafts, their elements, the row, the token) the small ones.
 #include "wdp_common.h"
 
 namespace wdp {
 namespace {
 
 constexpr int kPiece = 4096;   // elements that a workgroup of 256 sums in the form with two launches
-constexpr int kMaxDrafts = 64; // one wave tests them
-constexpr int kLaneVocab = 16; // largest vocabulary of the form with a lane a sequence
+constexpr int kMaxDrafts = 64;
 
 struct VerifyArgs {
   const void *target, *draft;
   const int32_t *drafts_in, *lengths;
   const float* u;
   int32_t *accepted, *tokens;
-  double* sums;  // [batch][pieces][2]: of r, of max(p, 0)
+  double* sums;  // [batch][pieces][2]: of r, of max(p, 0); behind them int32 [batch]: accepted
   int64_t start, batch;  // sequences [start, batch) of this launch
   int64_t target_batch, target_row, draft_batch, draft_row;
   int32_t drafts, vocab, bonus, pieces;
@@ -70,75 +70,152 @@ __device__ __forceinline__ void write_tokens(const VerifyArgs& a, int64_t s, int
 }
 
 // ---- a lane a sequence ----------------------------------------------------------------------
-template <typename T> __global__ __launch_bounds__(256) void verify_lane_kernel(VerifyArgs a) {
+// ONE: one draft and no bonus row, so that both rows are known beforehand and the test takes its elements from them.
+template <typename T, int MOST, bool ONE> __global__ __launch_bounds__(256) void verify_lane_kernel(VerifyArgs a) {
   const int64_t s = a.start + int64_t(blockIdx.x) * 256 + threadIdx.x;
   if (s >= a.batch) return;
   const int n = drafted(a, s);
-  int accepted = 0;
-  while (accepted < n && accepts<T>(a, s, accepted, a.drafts_in[s * a.drafts + accepted])) ++accepted;
-  const T *p, *q;
-  int token = -1;
-  if (draw_rows(a, s, accepted, n, &p, &q)) {
-    double sum = 0.0, plain = 0.0;
-    for (int j = 0; j < a.vocab; ++j) {
-      const double v = to_float(p[j]);
-      sum += positive(q ? v - double(to_float(q[j])) : v);
-      plain += positive(v);
+  float p[MOST], q[MOST];
+  const auto load = [&](const T* from_p, const T* from_q) {
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) {
+      p[j] = j < a.vocab ? to_float(from_p[j]) : 0.0f;
+      q[j] = j < a.vocab && from_q ? to_float(from_q[j]) : 0.0f;
     }
-    if (!(sum > 0.0)) q = nullptr, sum = plain;
+  };
+  int accepted = 0, first = -1;
+  bool draws;
+  if (ONE) {
+    first = a.drafts_in[s];
+    const double u = a.u[2 * s];
+    load(static_cast<const T*>(a.target) + s * a.target_batch, static_cast<const T*>(a.draft) + s * a.draft_batch);
+    float px = 0.0f, qx = 1.0f;  // (a token out of range is refused)
+#pragma unroll
+    for (int j = 0; j < MOST; ++j)
+      if (j == first && j < a.vocab) px = p[j], qx = q[j];
+    accepted = n == 1 && first >= 0 && first < a.vocab && u * double(qx) < double(px);
+    draws = accepted < n;
+  } else {
+    while (accepted < n && accepts<T>(a, s, accepted, a.drafts_in[s * a.drafts + accepted])) ++accepted;
+    const T *from_p, *from_q;
+    draws = draw_rows(a, s, accepted, n, &from_p, &from_q);
+    if (draws) load(from_p, from_q);
+  }
+  int token = -1;
+  if (draws) {
+    double r[MOST], sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) r[j] = positive(double(p[j]) - double(q[j])), sum += r[j];
+    if (!(sum > 0.0)) {  // nothing is left of p - q: from p itself
+      sum = 0.0;
+#pragma unroll
+      for (int j = 0; j < MOST; ++j) r[j] = positive(double(p[j])), sum += r[j];
+    }
     const double mark = double(a.u[s * (a.drafts + 1) + a.drafts]) * sum;
     double run = 0.0;
+    bool found = false;
     token = a.vocab - 1;
-    for (int j = 0; j < a.vocab; ++j) {
-      const double v = to_float(p[j]), r = positive(q ? v - double(to_float(q[j])) : v);
-      if (!(r > 0.0)) continue;
-      run += r;
-      token = j;
-      if (run > mark) break;
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) {
+      run += r[j];
+      if (!found && r[j] > 0.0) token = j, found = run > mark;
     }
   }
-  write_tokens(a, s, accepted, token, 0, 1);
+  if (ONE) {
+    a.tokens[s] = accepted ? first : token;
+    if (a.accepted) a.accepted[s] = accepted;
+  } else {
+    write_tokens(a, s, accepted, token, 0, 1);
+  }
 }
 
 // ---- a workgroup's search for the token within elements [at, at + 16 * threads) -----------------
-// r[16]: the lane's adjacent elements; before: sum of everything in front of them.  Lanes' sums are scanned over the
-// workgroup; the first element whose running sum passes the mark wins, else the last that is above zero.
+// r: the lane's adjacent elements.  Lanes' sums are scanned over the workgroup; the first element whose running sum passes
+// the mark wins, else the last that is above zero.
 constexpr int kEach = 16;
 
-template <typename T>
-__device__ __forceinline__ void load_rest(const T* p, const T* q, int first, int vocab, double r[kEach], double* plain) {
+template <typename T, int E>
+__device__ __forceinline__ void load_rest(const T* p, const T* q, int first, int vocab, double r[E], double* plain) {
+  constexpr int kStep = E < 8 ? E : 8;
   *plain = 0.0;
 #pragma unroll
-  for (int h = 0; h < kEach; h += 8) {
-    float pv[8], qv[8];
+  for (int h = 0; h < E; h += kStep) {
+    float pv[kStep], qv[kStep];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) pv[i] = qv[i] = 0.0f;
+    for (int i = 0; i < kStep; ++i) pv[i] = qv[i] = 0.0f;
     if (first + h < vocab) {
-      load_some<T, 8>(p + first + h, vocab - first - h, pv);
-      if (q) load_some<T, 8>(q + first + h, vocab - first - h, qv);
+      load_some<T, kStep>(p + first + h, vocab - first - h, pv);
+      if (q) load_some<T, kStep>(q + first + h, vocab - first - h, qv);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < kStep; ++i) {
       r[h + i] = positive(double(pv[i]) - double(qv[i]));
       *plain += positive(double(pv[i]));
     }
   }
 }
 
-__device__ __forceinline__ double shuffle_up(double v, int by) { return __shfl_up(v, by); }
-
-// Inclusive scan over the workgroup's lanes; *total: the sum.  Two barriers (waves > 1).
-template <int WAVES> __device__ __forceinline__ double scan(double v, double* places, double* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Inclusive scan over aligned groups of G lanes.
+template <int G> __device__ __forceinline__ double group_scan(double v) {
+  const int lane = threadIdx.x & (G - 1);
 #pragma unroll
-  for (int by = 1; by < 64; by <<= 1) {
-    const double left = shuffle_up(v, by);
+  for (int by = 1; by < G; by <<= 1) {
+    const double left = __shfl_up(v, by, G);
     if (lane >= by) v += left;
   }
-  if (WAVES == 1) {
-    *total = __shfl(v, 63);
-    return v;
+  return v;
+}
+
+// ---- G lanes a sequence, E adjacent elements of the row each -----------------------------------------
+template <typename T, int G, int E> __global__ __launch_bounds__(256) void verify_group_kernel(VerifyArgs a) {
+  const int64_t s = a.start + int64_t(blockIdx.x) * (256 / G) + threadIdx.x / G;
+  if (s >= a.batch) return;
+  const int lane = threadIdx.x & (G - 1), shift = threadIdx.x & 63 & ~(G - 1);
+  const auto votes = [&](bool yes) { return (__ballot(yes) >> shift) & (~uint64_t(0) >> (64 - G)); };  // of the group
+  const int n = drafted(a, s);
+  int accepted = 0;
+  for (int at = 0; at < n; at += G) {
+    const bool ok = at + lane < n && accepts<T>(a, s, at + lane, a.drafts_in[s * a.drafts + at + lane]);
+    const uint64_t refused = votes(!ok);
+    accepted = at + (refused ? __builtin_ctzll(refused) : G);
+    if (refused) break;
   }
+  const T *p, *q;
+  int token = -1;
+  if (draw_rows(a, s, accepted, n, &p, &q)) {
+    const int first = lane * E;
+    double r[E], plain, own = 0.0;
+    load_rest<T, E>(p, q, first, a.vocab, r, &plain);
+#pragma unroll
+    for (int i = 0; i < E; ++i) own += r[i];
+    double behind = group_scan<G>(own), sum = __shfl(behind, G - 1, G);
+    if (!(sum > 0.0) && q) {  // nothing is left of p - q: from p itself
+      load_rest<T, E>(p, static_cast<const T*>(nullptr), first, a.vocab, r, &own);
+      behind = group_scan<G>(own), sum = __shfl(behind, G - 1, G);
+    }
+    const double mark = double(a.u[s * (a.drafts + 1) + a.drafts]) * sum;
+    double run = behind - own;
+    int hit = -1, last = -1;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      run += r[i];
+      if (r[i] > 0.0) {
+        last = first + i;
+        if (hit < 0 && run > mark) hit = first + i;
+      }
+    }
+    const uint64_t hits = votes(hit >= 0), some = votes(last >= 0);
+    token = a.vocab - 1;
+    if (hits) token = __shfl(hit, __builtin_ctzll(hits), G);
+    else if (some) token = __shfl(last, 63 - __builtin_clzll(some), G);
+  }
+  write_tokens(a, s, accepted, token, lane, G);
+}
+
+// Inclusive scan over the workgroup's lanes; *total: the sum.  Two barriers.
+template <int WAVES> __device__ __forceinline__ double scan(double v, double* places, double* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  v = group_scan<64>(v);
   __syncthreads();
   if (lane == 63) places[wave] = v;
   __syncthreads();
@@ -173,7 +250,7 @@ template <int WAVES> __device__ __forceinline__ int find(const double r[kEach], 
   return best[0] != 0x7FFFFFFF ? best[0] : best[1];
 }
 
-// ---- a workgroup (or wave) a sequence: the whole row in registers -------------------------------------
+// ---- a workgroup a sequence: the whole row in registers -------------------------------------
 template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES) void verify_row_kernel(VerifyArgs a) {
   __shared__ double places[WAVES];
   __shared__ int best[2];
@@ -185,12 +262,12 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES) void v
   if (draw_rows(a, s, accepted, n, &p, &q)) {
     const int first = threadIdx.x * kEach;
     double r[kEach], plain, sum, own = 0.0;
-    load_rest<T>(p, q, first, a.vocab, r, &plain);
+    load_rest<T, kEach>(p, q, first, a.vocab, r, &plain);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) own += r[i];
     double behind = scan<WAVES>(own, places, &sum);
     if (!(sum > 0.0) && q) {  // nothing is left of p - q: from p itself
-      load_rest<T>(p, static_cast<const T*>(nullptr), first, a.vocab, r, &own);
+      load_rest<T, kEach>(p, static_cast<const T*>(nullptr), first, a.vocab, r, &own);
       behind = scan<WAVES>(own, places, &sum);
     }
     token = find<WAVES>(r, behind, own, double(a.u[s * (a.drafts + 1) + a.drafts]) * sum, first, best);
@@ -201,62 +278,80 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES) void v
 }
 
 // ---- long rows: sums of the pieces, then the search in one of them --------------------------------------
-template <typename T> __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a) {
+__device__ __forceinline__ int32_t* counts(const VerifyArgs& a, int64_t all) { return reinterpret_cast<int32_t*>(a.sums + all * a.pieces * 2); }
+
+template <typename T> __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, int64_t all) {
   __shared__ double places[4];
   const int64_t s = a.start + blockIdx.y + int64_t(blockIdx.z) * 32768;
   if (s >= a.batch) return;
   const int n = drafted(a, s), accepted = count_accepted<T>(a, s, n);
+  if (blockIdx.x == 0 && threadIdx.x == 0) counts(a, all)[s] = accepted;
   const T *p, *q;
   if (!draw_rows(a, s, accepted, n, &p, &q)) return;
-  double r[kEach], plain, sum, all, own = 0.0;
-  load_rest<T>(p, q, blockIdx.x * kPiece + threadIdx.x * kEach, a.vocab, r, &plain);
+  double r[kEach], plain, sum, total, own = 0.0;
+  load_rest<T, kEach>(p, q, blockIdx.x * kPiece + threadIdx.x * kEach, a.vocab, r, &plain);
 #pragma unroll
   for (int i = 0; i < kEach; ++i) own += r[i];
   scan<4>(own, places, &sum);
-  scan<4>(plain, places, &all);
+  scan<4>(plain, places, &total);
   if (threadIdx.x == 0) {
     a.sums[(s * a.pieces + blockIdx.x) * 2] = sum;
-    a.sums[(s * a.pieces + blockIdx.x) * 2 + 1] = all;
+    a.sums[(s * a.pieces + blockIdx.x) * 2 + 1] = total;
   }
 }
 
-template <typename T> __global__ __launch_bounds__(256) void verify_find_kernel(VerifyArgs a) {
+template <typename T> __global__ __launch_bounds__(256) void verify_find_kernel(VerifyArgs a, int64_t all) {
   __shared__ double places[4];
   __shared__ int best[2];
   const int64_t s = a.start + blockIdx.x;
-  const int n = drafted(a, s), accepted = count_accepted<T>(a, s, n);
+  // everything that depends on nothing is asked for at once: the call's time is the chain of loads that do
+  const int lane = threadIdx.x & 63, slots = a.drafts + a.bonus;
+  const double* sums = a.sums + s * a.pieces * 2;
+  const double first_sum = lane < a.pieces ? sums[2 * lane] : 0.0, first_plain = lane < a.pieces ? sums[2 * lane + 1] : 0.0;
+  const double u = a.u[s * (a.drafts + 1) + a.drafts];
+  const int kept = int(threadIdx.x) < a.drafts ? a.drafts_in[s * a.drafts + threadIdx.x] : -1;  // (at most 64)
+  const int n = drafted(a, s), accepted = counts(a, all)[s];
   const T *p, *q;
   int token = -1;
   if (draw_rows(a, s, accepted, n, &p, &q)) {
-    // the row's sum, and the piece: every lane goes through the pieces' sums (the same order in all)
-    const double* sums = a.sums + s * a.pieces * 2;
-    double total = 0.0, plain = 0.0;
-    for (int i = 0; i < a.pieces; ++i) total += sums[2 * i], plain += sums[2 * i + 1];
+    // the row's sum and the piece, by each wave for itself: 64 pieces at a time
+    double total = first_sum, plain = first_plain;
+    for (int at = 64; at < a.pieces; at += 64) {
+      const bool some = at + lane < a.pieces;
+      total += some ? sums[2 * (at + lane)] : 0.0, plain += some ? sums[2 * (at + lane) + 1] : 0.0;
+    }
+    total = __shfl(group_scan<64>(total), 63), plain = __shfl(group_scan<64>(plain), 63);
     const bool from_p = !(total > 0.0) && q;
     if (from_p) total = plain, q = nullptr;
-    const double mark = double(a.u[s * (a.drafts + 1) + a.drafts]) * total;
+    const double mark = u * total;
     double run = 0.0, before = 0.0;
     int piece = -1;
-    for (int i = 0; i < a.pieces; ++i) {
-      const double v = sums[2 * i + (from_p ? 1 : 0)];
-      if (!(v > 0.0)) continue;
-      piece = i, before = run;
-      run += v;
-      if (run > mark) break;
+    for (int at = 0; at < a.pieces; at += 64) {
+      double v = 0.0;
+      if (at == 0) v = from_p ? first_plain : first_sum;
+      else if (at + lane < a.pieces) v = sums[2 * (at + lane) + (from_p ? 1 : 0)];
+      const double behind = run + group_scan<64>(v);
+      const uint64_t some = __ballot(v > 0.0), hits = __ballot(v > 0.0 && behind > mark);
+      if (hits || some) {
+        const int l = hits ? __builtin_ctzll(hits) : 63 - __builtin_clzll(some);
+        piece = at + l, before = __shfl(behind - v, l);
+      }
+      if (hits) break;
+      run = __shfl(behind, 63);
     }
     if (piece >= 0) {
       const int first = piece * kPiece + threadIdx.x * kEach;
-      double r[kEach], unused, all, own = 0.0;
-      load_rest<T>(p, q, first, a.vocab, r, &unused);
+      double r[kEach], unused, sum, own = 0.0;
+      load_rest<T, kEach>(p, q, first, a.vocab, r, &unused);
 #pragma unroll
       for (int i = 0; i < kEach; ++i) own += r[i];
-      const double behind = scan<4>(own, places, &all) + before;
+      const double behind = scan<4>(own, places, &sum) + before;
       token = find<4>(r, behind, own, mark, first, best);
     }
     if (token < 0) token = a.vocab - 1;
   }
-  __syncthreads();
-  write_tokens(a, s, accepted, token, threadIdx.x, 256);
+  if (int(threadIdx.x) < slots) a.tokens[s * slots + threadIdx.x] = int(threadIdx.x) < accepted ? kept : int(threadIdx.x) == accepted ? token : -1;
+  if (threadIdx.x == 0 && a.accepted) a.accepted[s] = accepted;
 }
 
 // (a launch takes 2^22 sequences: all sizes of a grid stay far from their limits)
@@ -265,12 +360,16 @@ template <typename T> void launch(VerifyArgs a, hipStream_t stream) {
   for (; a.start < end; a.start += most) {
     a.batch = end - a.start < most ? end : a.start + most;
     const unsigned count = unsigned(a.batch - a.start);
-    if (a.vocab <= kLaneVocab) verify_lane_kernel<T><<<dim3((count + 255) / 256), 256, 0, stream>>>(a);
-    else if (a.vocab <= 64 * kEach) verify_row_kernel<T, 1><<<dim3(count), 64, 0, stream>>>(a);
+    const auto blocks = [&](unsigned each) { return dim3((count + each - 1) / each); };
+    if (a.vocab <= 8 && a.drafts == 1 && !a.bonus) verify_lane_kernel<T, 8, true><<<blocks(256), 256, 0, stream>>>(a);
+    else if (a.vocab <= 8) verify_lane_kernel<T, 8, false><<<blocks(256), 256, 0, stream>>>(a);
+    else if (a.vocab <= 64) verify_group_kernel<T, 16, 4><<<blocks(16), 256, 0, stream>>>(a);
+    else if (a.vocab <= 256) verify_group_kernel<T, 64, 4><<<blocks(4), 256, 0, stream>>>(a);
+    else if (a.vocab <= 1024) verify_group_kernel<T, 64, 16><<<blocks(4), 256, 0, stream>>>(a);
     else if (a.vocab <= kPiece) verify_row_kernel<T, 4><<<dim3(count), 256, 0, stream>>>(a);
     else {
-      verify_sums_kernel<T><<<dim3(unsigned(a.pieces), count < 32768 ? count : 32768, (count + 32767) / 32768), 256, 0, stream>>>(a);
-      verify_find_kernel<T><<<dim3(count), 256, 0, stream>>>(a);
+      verify_sums_kernel<T><<<dim3(unsigned(a.pieces), count < 32768 ? count : 32768, (count + 32767) / 32768), 256, 0, stream>>>(a, end);
+      verify_find_kernel<T><<<dim3(count), 256, 0, stream>>>(a, end);
     }
   }
 }
@@ -297,7 +396,8 @@ int wdp_verify_workspace(const wdp_verify_config* cfg, size_t* bytes) {
   if (!cfg || !bytes) return WD_E_NULL;
   const int rc = wdp::check(*cfg);
   if (rc != WD_OK) return rc;
-  *bytes = size_t(cfg->batch) * size_t(wdp::pieces_of(*cfg)) * 2 * sizeof(double);
+  const size_t pieces = size_t(wdp::pieces_of(*cfg));
+  *bytes = pieces ? size_t(cfg->batch) * (pieces * 2 * sizeof(double) + sizeof(int32_t)) : 0;
   return WD_OK;
 }
 
