@@ -6,7 +6,7 @@
 // the row's sum, so that the kernels below, which sum in different orders, answer alike.
 //
 // Forms by the vocabulary.  Few actions (a policy of Tag has five): a lane a sequence, the row in its registers.  Up to
-// 1024: sixteen lanes or a wave a sequence, no barrier.  Up to 4096: a workgroup.  Longer rows: a workgroup a piece of 4096
+// 1024: sixteen lanes or a wave a sequence, no barrier.  Up to 4096: a workgroup.  Longer rows: a wave a piece of 1024
 // elements sums it, a second launch finds the piece that holds the drawn token and goes through that one alone.  Memory
 // bounds the large batches, the chain of dependent loads (drafts, their elements, the row, the token) the small ones.
 #include "wdp_common.h"
@@ -14,7 +14,8 @@
 namespace wdp {
 namespace {
 
-constexpr int kPiece = 4096;   // elements that a workgroup of 256 sums in the form with two launches
+constexpr int kRow = 4096;     // largest vocabulary that a workgroup of 256 holds in registers
+constexpr int kPiece = 1024;   // elements that a wave sums in the form with two launches
 constexpr int kMaxDrafts = 64;
 
 struct VerifyArgs {
@@ -155,15 +156,50 @@ __device__ __forceinline__ void load_rest(const T* p, const T* q, int first, int
   }
 }
 
-// Inclusive scan over aligned groups of G lanes.
+// Inclusive scan over aligned groups of G = 16 or 64 lanes (all of them active): within a row of sixteen lanes by shifts
+// that need no LDS, then the sums of the rows before.
+template <int BY> __device__ __forceinline__ double from_left(double v) {  // zero where there is no such lane in the row
+  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, int(bits), 0x110 + BY, 0xF, 0xF, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, int(bits >> 32), 0x110 + BY, 0xF, 0xF, true);
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+__device__ __forceinline__ double of_lane(double v, int lane) {
+  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane(int(bits), lane), hi = __builtin_amdgcn_readlane(int(bits >> 32), lane);
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
 template <int G> __device__ __forceinline__ double group_scan(double v) {
-  const int lane = threadIdx.x & (G - 1);
-#pragma unroll
-  for (int by = 1; by < G; by <<= 1) {
-    const double left = __shfl_up(v, by, G);
-    if (lane >= by) v += left;
+  static_assert(G == 16 || G == 64, "a row of lanes, or the wave");
+  v += from_left<1>(v);
+  v += from_left<2>(v);
+  v += from_left<4>(v);
+  v += from_left<8>(v);
+  if (G == 64) {
+    const int row = (threadIdx.x >> 4) & 3;
+    const double a = of_lane(v, 15), b = of_lane(v, 31), c = of_lane(v, 47);
+    v += row == 0 ? 0.0 : row == 1 ? a : row == 2 ? a + b : a + b + c;
   }
   return v;
+}
+// The group's last lane's value, in all of them.
+template <int G> __device__ __forceinline__ double last_of(double v) { return G == 64 ? of_lane(v, 63) : __shfl(v, G - 1, G); }
+
+// The token among a group's elements r (E adjacent ones a lane, from `first` on), `run` being the sum of everything before
+// the lane's: the first above zero whose running sum passes the mark, else the last above zero, else -1.
+template <int G, int E, typename Votes> __device__ __forceinline__ int find_in_group(const double r[E], double run, double mark, int first, Votes votes) {
+  int hit = -1, last = -1;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    run += r[i];
+    if (r[i] > 0.0) {
+      last = first + i;
+      if (hit < 0 && run > mark) hit = first + i;
+    }
+  }
+  const uint64_t hits = votes(hit >= 0), some = votes(last >= 0);
+  if (hits) return __shfl(hit, __builtin_ctzll(hits), G);
+  return some ? __shfl(last, 63 - __builtin_clzll(some), G) : -1;
 }
 
 // ---- G lanes a sequence, E adjacent elements of the row each -----------------------------------------
@@ -188,26 +224,14 @@ template <typename T, int G, int E> __global__ __launch_bounds__(256) void verif
     load_rest<T, E>(p, q, first, a.vocab, r, &plain);
 #pragma unroll
     for (int i = 0; i < E; ++i) own += r[i];
-    double behind = group_scan<G>(own), sum = __shfl(behind, G - 1, G);
+    double behind = group_scan<G>(own), sum = last_of<G>(behind);
     if (!(sum > 0.0) && q) {  // nothing is left of p - q: from p itself
       load_rest<T, E>(p, static_cast<const T*>(nullptr), first, a.vocab, r, &own);
-      behind = group_scan<G>(own), sum = __shfl(behind, G - 1, G);
+      behind = group_scan<G>(own), sum = last_of<G>(behind);
     }
     const double mark = double(a.u[s * (a.drafts + 1) + a.drafts]) * sum;
-    double run = behind - own;
-    int hit = -1, last = -1;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      run += r[i];
-      if (r[i] > 0.0) {
-        last = first + i;
-        if (hit < 0 && run > mark) hit = first + i;
-      }
-    }
-    const uint64_t hits = votes(hit >= 0), some = votes(last >= 0);
-    token = a.vocab - 1;
-    if (hits) token = __shfl(hit, __builtin_ctzll(hits), G);
-    else if (some) token = __shfl(last, 63 - __builtin_clzll(some), G);
+    token = find_in_group<G, E>(r, behind - own, mark, first, votes);
+    if (token < 0) token = a.vocab - 1;
   }
   write_tokens(a, s, accepted, token, lane, G);
 }
@@ -281,48 +305,46 @@ template <typename T, int WAVES> __global__ __launch_bounds__(64 * WAVES) void v
 __device__ __forceinline__ int32_t* counts(const VerifyArgs& a, int64_t all) { return reinterpret_cast<int32_t*>(a.sums + all * a.pieces * 2); }
 
 template <typename T> __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, int64_t all) {
-  __shared__ double places[4];
   const int64_t s = a.start + blockIdx.y + int64_t(blockIdx.z) * 32768;
   if (s >= a.batch) return;
   const int n = drafted(a, s), accepted = count_accepted<T>(a, s, n);
   if (blockIdx.x == 0 && threadIdx.x == 0) counts(a, all)[s] = accepted;
+  const int piece = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   const T *p, *q;
-  if (!draw_rows(a, s, accepted, n, &p, &q)) return;
-  double r[kEach], plain, sum, total, own = 0.0;
-  load_rest<T, kEach>(p, q, blockIdx.x * kPiece + threadIdx.x * kEach, a.vocab, r, &plain);
+  if (piece >= a.pieces || !draw_rows(a, s, accepted, n, &p, &q)) return;
+  double r[kEach], plain, own = 0.0;
+  load_rest<T, kEach>(p, q, piece * kPiece + lane * kEach, a.vocab, r, &plain);
 #pragma unroll
   for (int i = 0; i < kEach; ++i) own += r[i];
-  scan<4>(own, places, &sum);
-  scan<4>(plain, places, &total);
-  if (threadIdx.x == 0) {
-    a.sums[(s * a.pieces + blockIdx.x) * 2] = sum;
-    a.sums[(s * a.pieces + blockIdx.x) * 2 + 1] = total;
+  own = group_scan<64>(own), plain = group_scan<64>(plain);
+  if (lane == 63) {
+    a.sums[(s * a.pieces + piece) * 2] = own;
+    a.sums[(s * a.pieces + piece) * 2 + 1] = plain;
   }
 }
 
-template <typename T> __global__ __launch_bounds__(256) void verify_find_kernel(VerifyArgs a, int64_t all) {
-  __shared__ double places[4];
-  __shared__ int best[2];
+template <typename T> __global__ __launch_bounds__(64) void verify_find_kernel(VerifyArgs a, int64_t all) {
   const int64_t s = a.start + blockIdx.x;
   // everything that depends on nothing is asked for at once: the call's time is the chain of loads that do
-  const int lane = threadIdx.x & 63, slots = a.drafts + a.bonus;
+  const int lane = threadIdx.x, slots = a.drafts + a.bonus;
   const double* sums = a.sums + s * a.pieces * 2;
   const double first_sum = lane < a.pieces ? sums[2 * lane] : 0.0, first_plain = lane < a.pieces ? sums[2 * lane + 1] : 0.0;
   const double u = a.u[s * (a.drafts + 1) + a.drafts];
-  const int kept = int(threadIdx.x) < a.drafts ? a.drafts_in[s * a.drafts + threadIdx.x] : -1;  // (at most 64)
+  const int kept = lane < a.drafts ? a.drafts_in[s * a.drafts + lane] : -1;  // (at most 64)
   const int n = drafted(a, s), accepted = counts(a, all)[s];
   const T *p, *q;
   int token = -1;
   if (draw_rows(a, s, accepted, n, &p, &q)) {
     // the row's sum and the piece, by each wave for itself: 64 pieces at a time
-    double total = first_sum, plain = first_plain;
-    for (int at = 64; at < a.pieces; at += 64) {
-      const bool some = at + lane < a.pieces;
-      total += some ? sums[2 * (at + lane)] : 0.0, plain += some ? sums[2 * (at + lane) + 1] : 0.0;
-    }
-    total = __shfl(group_scan<64>(total), 63), plain = __shfl(group_scan<64>(plain), 63);
+    double total = first_sum;
+    for (int at = 64; at < a.pieces; at += 64) total += at + lane < a.pieces ? sums[2 * (at + lane)] : 0.0;
+    total = of_lane(group_scan<64>(total), 63);
     const bool from_p = !(total > 0.0) && q;
-    if (from_p) total = plain, q = nullptr;
+    if (from_p) {
+      q = nullptr, total = first_plain;
+      for (int at = 64; at < a.pieces; at += 64) total += at + lane < a.pieces ? sums[2 * (at + lane) + 1] : 0.0;
+      total = of_lane(group_scan<64>(total), 63);
+    }
     const double mark = u * total;
     double run = 0.0, before = 0.0;
     int piece = -1;
@@ -334,24 +356,25 @@ template <typename T> __global__ __launch_bounds__(256) void verify_find_kernel(
       const uint64_t some = __ballot(v > 0.0), hits = __ballot(v > 0.0 && behind > mark);
       if (hits || some) {
         const int l = hits ? __builtin_ctzll(hits) : 63 - __builtin_clzll(some);
-        piece = at + l, before = __shfl(behind - v, l);
+        piece = at + l, before = of_lane(behind - v, l);
       }
       if (hits) break;
-      run = __shfl(behind, 63);
+      run = of_lane(behind, 63);
     }
     if (piece >= 0) {
-      const int first = piece * kPiece + threadIdx.x * kEach;
-      double r[kEach], unused, sum, own = 0.0;
+      const int first = piece * kPiece + lane * kEach;
+      double r[kEach], unused, own = 0.0;
       load_rest<T, kEach>(p, q, first, a.vocab, r, &unused);
 #pragma unroll
       for (int i = 0; i < kEach; ++i) own += r[i];
-      const double behind = scan<4>(own, places, &sum) + before;
-      token = find<4>(r, behind, own, mark, first, best);
+      const double behind = group_scan<64>(own) + before;
+      token = find_in_group<64, kEach>(r, behind - own, mark, first, [](bool yes) { return uint64_t(__ballot(yes)); });
     }
     if (token < 0) token = a.vocab - 1;
   }
-  if (int(threadIdx.x) < slots) a.tokens[s * slots + threadIdx.x] = int(threadIdx.x) < accepted ? kept : int(threadIdx.x) == accepted ? token : -1;
-  if (threadIdx.x == 0 && a.accepted) a.accepted[s] = accepted;
+  // (65 slots at most: drafts and one more)
+  for (int i = lane; i < slots; i += 64) a.tokens[s * slots + i] = i < accepted ? kept : i == accepted ? token : -1;
+  if (lane == 0 && a.accepted) a.accepted[s] = accepted;
 }
 
 // (a launch takes 2^22 sequences: all sizes of a grid stay far from their limits)
@@ -366,15 +389,15 @@ template <typename T> void launch(VerifyArgs a, hipStream_t stream) {
     else if (a.vocab <= 64) verify_group_kernel<T, 16, 4><<<blocks(16), 256, 0, stream>>>(a);
     else if (a.vocab <= 256) verify_group_kernel<T, 64, 4><<<blocks(4), 256, 0, stream>>>(a);
     else if (a.vocab <= 1024) verify_group_kernel<T, 64, 16><<<blocks(4), 256, 0, stream>>>(a);
-    else if (a.vocab <= kPiece) verify_row_kernel<T, 4><<<dim3(count), 256, 0, stream>>>(a);
+    else if (a.vocab <= kRow) verify_row_kernel<T, 4><<<dim3(count), 256, 0, stream>>>(a);
     else {
-      verify_sums_kernel<T><<<dim3(unsigned(a.pieces), count < 32768 ? count : 32768, (count + 32767) / 32768), 256, 0, stream>>>(a, end);
-      verify_find_kernel<T><<<dim3(count), 256, 0, stream>>>(a, end);
+      verify_sums_kernel<T><<<dim3(unsigned((a.pieces + 3) / 4), count < 32768 ? count : 32768, (count + 32767) / 32768), 256, 0, stream>>>(a, end);
+      verify_find_kernel<T><<<dim3(count), 64, 0, stream>>>(a, end);
     }
   }
 }
 
-int pieces_of(const wdp_verify_config& c) { return c.vocab <= kPiece ? 0 : (c.vocab + kPiece - 1) / kPiece; }
+int pieces_of(const wdp_verify_config& c) { return c.vocab <= kRow ? 0 : (c.vocab + kPiece - 1) / kPiece; }
 
 int check(const wdp_verify_config& c) {
   if (c.struct_size != sizeof(wdp_verify_config) || !is_float_type(c.type)) return WD_E_CONFIG;
