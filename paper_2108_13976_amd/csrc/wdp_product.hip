@@ -289,10 +289,21 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(ProductAr
 
 // ---- large tiles -----------------------------------------------------------------------------------------
 // Rows at 16-byte boundaries: the chunks go from memory to LDS without registers between (a wave's instruction fills
-// 1 KB, eight rows; the lane that fills a place asks for the chunk that belongs there).  256 x 256 with eight waves of
-// 128 x 64: a block needs 2048 cycles of a SIMD's matrix core, 1536 of LDS for the fragments and 512 for the chunks.
+// 1 KB, eight rows; the lane that fills a place asks for the chunk that belongs there), a block ahead.
+//
+// 256 x 256 with eight waves of 128 x 64: a block is 2048 cycles of a SIMD's matrix core beside 1024 of its vector
+// unit; LDS is in use for a seventh of the time (no bank conflicts).  The results of an instruction are added three
+// instructions later, or the wave stands still for the matrix core's latency (8192 x 8192 x 4096: 304 us against 283).
+// Without its loads that product takes 249 us, of which 27 are c's 128 MB at a copy's rate: the matrix core, slowed by
+// its clock, is what is left.  Two blocks ahead or three (with fewer workgroups a CU) are slower for every size.
+//
+// Scales: without ROWS (a wave's columns share one) they are requested into registers a block ahead; with ROWS, one for
+// each column, both kinds come by way of LDS (5000 x 333 x 1000 with float32 results: 13.2 us by registers, 11.6).
 __device__ __forceinline__ void to_lds(const uint8_t* from, i32x4* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+__device__ __forceinline__ void to_lds(const float* from, float* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
 }
 
 template <int FA, int FB, bool ROWS, typename C, int BM, int BN, int WM, int WN>
@@ -300,7 +311,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_large_kernel(ProductA
   constexpr bool EXACT = sizeof(C) == 4;
   constexpr int kWaves = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
   constexpr int kA = BM / 8 / kWaves, kB = BN / 8 / kWaves;  // eights of rows that a wave brings
+  static_assert(BM % 64 == 0 && BN % 64 == 0 && BM / 64 + BN / 64 <= kWaves, "a wave brings 64 scales at most");
   __shared__ i32x4 lds[2][(BM + BN) * 8];
+  __shared__ __attribute__((aligned(16))) float scales[2][ROWS ? BM + BN : 4];
   static_assert(sizeof(lds) >= kWaves * kLineBytes, "results are staged there");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int mt, nt;
@@ -326,26 +339,31 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_large_kernel(ProductA
     chunk_b[i & 1] = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
     from_b[i] = uint32_t(n0 + col < p.n ? col : p.n - 1 - n0) * uint32_t(p.b_stride) + chunk_b[i & 1];
   }
+  // without ROWS: the lane's rows' scales, and the wave's columns'
   const float* tile_sa = p.a_scale + int64_t(m0 + wm) * p.as_row;
   const uint32_t from_sa = uint32_t(r16) * uint32_t(p.as_row);
-  // scales of b: one for the wave's columns, or (ROWS) one for each column of the lane's results
-  const float* from_sb[ROWS ? TN : 1][ROWS ? 4 : 1];
-  float next_sa[TM], next_sb[ROWS ? TN : 1][ROWS ? 4 : 1];
-#pragma unroll
-  for (int j = 0; j < (ROWS ? TN : 1); ++j)
-#pragma unroll
-    for (int e = 0; e < (ROWS ? 4 : 1); ++e) {
-      const int col = n0 + wn + (ROWS ? column(j * 16 + g * 4 + e) : 0), at = col < p.n ? col : p.n - 1;
-      from_sb[j][e] = p.b_scale + int64_t(ROWS && p.by_row ? at : at / WDP_BLOCK) * p.bs_row;
-    }
+  const int first = n0 + wn < p.n ? n0 + wn : p.n - 1;
+  const float* from_sb = p.b_scale + int64_t(first / WDP_BLOCK) * p.bs_row;
+  float next_sa[TM], next_sb = 0.0f;
+  // with ROWS: the first waves bring those of a, the next those of b
+  const float* from_scale = nullptr;
+  int64_t scale_block = p.as_block;
+  if (ROWS && wave < BM / 64) {
+    from_scale = p.a_scale + int64_t(m0 + wave * 64 + lane) * p.as_row;
+  } else if (ROWS && wave < BM / 64 + BN / 64) {
+    const int col = n0 + column((wave - BM / 64) * 64 + lane), at = col < p.n ? col : p.n - 1;
+    from_scale = p.b_scale + int64_t(p.by_row ? at : at / WDP_BLOCK) * p.bs_row;
+    scale_block = p.bs_block;
+  }
   auto request = [&](int block, int half) {
     const int k0 = block * WDP_BLOCK;
+    if (ROWS) {
+      if (from_scale) to_lds(from_scale + block * scale_block, &scales[half][wave * 64]);
+    } else {
+      next_sb = from_sb[block * p.bs_block];
 #pragma unroll
-    for (int j = 0; j < (ROWS ? TN : 1); ++j)
-#pragma unroll
-      for (int e = 0; e < (ROWS ? 4 : 1); ++e) next_sb[j][e] = from_sb[j][e][block * p.bs_block];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) next_sa[i] = (tile_sa + block * p.as_block + i * 16 * p.as_row)[from_sa];
+      for (int i = 0; i < TM; ++i) next_sa[i] = (tile_sa + block * p.as_block + i * 16 * p.as_row)[from_sa];
+    }
     const uint8_t *a = tile_a + k0, *b = tile_b + k0;
     if (k0 + WDP_BLOCK <= p.k) {
 #pragma unroll
@@ -370,14 +388,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_large_kernel(ProductA
   request(0, 0);
   for (int block = 0; block < p.blocks; ++block) {
     const int half = block & 1;
-    float sa[TM], sb[ROWS ? TN : 1][ROWS ? 4 : 1];  // (without ROWS both are in sa)
+    float sa[TM];
     __syncthreads();  // this block's chunks have arrived, and everyone is through with the other half
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] = ROWS ? next_sa[i] : next_sa[i] * next_sb[0][0];
-#pragma unroll
-    for (int j = 0; j < (ROWS ? TN : 1); ++j)
-#pragma unroll
-      for (int e = 0; e < (ROWS ? 4 : 1); ++e) sb[j][e] = next_sb[j][e];
+    for (int i = 0; i < TM; ++i) sa[i] = ROWS ? scales[half][wm + i * 16 + r16] : next_sa[i] * next_sb;
     if (block + 1 < p.blocks) request(block + 1, half ^ 1);
     else if (p.k & (WDP_BLOCK - 1)) {
       // bytes beyond k: zeros
@@ -392,17 +406,18 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_large_kernel(ProductA
       __syncthreads();
     }
     Fragment<EXACT> fb[TN];
+    f32x4 sb[ROWS ? TN : 1];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       const int row = BM + wn + j * 16 + r16;
       fb[j] = fragment<FB, EXACT>(lds[half][place(row, g)], lds[half][place(row, g + 4)]);
+      if (ROWS) sb[j] = *reinterpret_cast<const f32x4*>(&scales[half][BM + wn + j * 16 + g * 4]);
     }
     auto load_a = [&](int i) {
       const int row = wm + i * 16 + r16;
       return fragment<FA, EXACT>(lds[half][place(row, g)], lds[half][place(row, g + 4)]);
     };
     constexpr int kDelay = 3;
-    // an instruction's results are added kDelay instructions later: the matrix core goes on meanwhile
     Fragment<EXACT> fa[2];
     fa[0] = load_a(0);
     f32x4 part[kDelay + 1];
@@ -416,7 +431,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_large_kernel(ProductA
       if (e >= kDelay) {
         const int d = e - kDelay;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) acc[d / TN][d % TN][x] = fmaf(part[d % (kDelay + 1)][x], ROWS ? sa[d / TN] * sb[ROWS ? d % TN : 0][ROWS ? x : 0] : sa[d / TN], acc[d / TN][d % TN][x]);
+        for (int x = 0; x < 4; ++x)
+          acc[d / TN][d % TN][x] = fmaf(part[d % (kDelay + 1)][x], ROWS ? sa[d / TN] * sb[ROWS ? d % TN : 0][x] : sa[d / TN], acc[d / TN][d % TN][x]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }

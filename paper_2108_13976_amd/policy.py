@@ -246,13 +246,13 @@ def rms_norm(x, weight=None, residual=None, eps=1e-5, out8=None, y=None, h=None)
     cfg, rows, want_y, q_shape, scale_shape, cut = plan
     empty = _torch().empty
     if residual is not None and h is None:
-        h = empty(x.shape, dtype=x.dtype, device=x.device)
+        h = _torch().empty_like(x) if x.is_contiguous() else empty(x.shape, dtype=x.dtype, device=x.device)
     rstd = empty(rows, dtype=_F32, device=x.device)
     out = empty(x.shape, dtype=x.dtype, device=x.device) if want_y else None
     q = scale = None
     if out8 is not None:
         q = empty(q_shape, dtype=out8, device=x.device)
-        scale = empty(scale_shape, dtype=_F32, device=x.device).t()
+        scale = _torch().empty_strided(scale_shape, (1, rows), dtype=_F32, device=x.device)
     _call(device, "wdp_norm", cfg, wdp_norm_buffers(
         x.data_ptr(), None if residual is None else residual.data_ptr(), None if weight is None else weight.data_ptr(),
         None if h is None else h.data_ptr(), out.data_ptr() if want_y else None, None if q is None else q.data_ptr(),
@@ -288,7 +288,7 @@ def _plan_norm(key, x, weight, residual, eps, out8, y, h):
     cfg = wdp_norm_config(ctypes.sizeof(wdp_norm_config), floats[x.dtype], WDP_F32 if weight is None else floats[weight.dtype],
                           eights[out8] if out8 is not None else 0, rows, width, eps, x_stride, residual_stride, h_stride, width, q_stride,
                           1, rows, 0, 0, 0, _gpu(what, key))
-    return _keep(key, (cfg, rows, want_y, (rows, q_stride), (blocks, rows), width if out8 is not None and q_stride != width else None))
+    return _keep(key, (cfg, rows, want_y, (rows, q_stride), (rows, blocks), width if out8 is not None and q_stride != width else None))
 
 
 def rms_norm_backward(dy, h, weight, rstd, dh=None, want_dw=True):
