@@ -299,6 +299,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(ProductAr
 //
 // Scales: without ROWS (a wave's columns share one) they are requested into registers a block ahead; with ROWS, one for
 // each column, both kinds come by way of LDS (5000 x 333 x 1000 with float32 results: 13.2 us by registers, 11.6).
+__device__ const i32x4 kZeros = {0, 0, 0, 0};
 __device__ __forceinline__ void to_lds(const uint8_t* from, i32x4* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
@@ -371,13 +372,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_large_kernel(ProductA
 #pragma unroll
       for (int i = 0; i < kB; ++i) to_lds(b + from_b[i], &lds[half][BM * 8 + (wave * kB + i) * 64]);
     } else {
-      // the last block's end: chunks with nothing of the row stay out (what they hold is cleared below)
+      // the last block's end: zeros in place of chunks with nothing of the row
 #pragma unroll
-      for (int i = 0; i < kA; ++i)
-        if (k0 + chunk_a[i & 1] < p.k) to_lds(a + from_a[i], &lds[half][(wave * kA + i) * 64]);
+      for (int i = 0; i < kA; ++i) to_lds(k0 + chunk_a[i & 1] < p.k ? a + from_a[i] : reinterpret_cast<const uint8_t*>(&kZeros), &lds[half][(wave * kA + i) * 64]);
 #pragma unroll
-      for (int i = 0; i < kB; ++i)
-        if (k0 + chunk_b[i & 1] < p.k) to_lds(b + from_b[i], &lds[half][BM * 8 + (wave * kB + i) * 64]);
+      for (int i = 0; i < kB; ++i) to_lds(k0 + chunk_b[i & 1] < p.k ? b + from_b[i] : reinterpret_cast<const uint8_t*>(&kZeros), &lds[half][BM * 8 + (wave * kB + i) * 64]);
     }
   };
   f32x4 acc[TM][TN];
@@ -393,15 +392,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_large_kernel(ProductA
 #pragma unroll
     for (int i = 0; i < TM; ++i) sa[i] = ROWS ? scales[half][wm + i * 16 + r16] : next_sa[i] * next_sb;
     if (block + 1 < p.blocks) request(block + 1, half ^ 1);
-    else if (p.k & (WDP_BLOCK - 1)) {
-      // bytes beyond k: zeros
-      const int left = p.k & (WDP_BLOCK - 1);
-      for (int e = threadIdx.x; e < (BM + BN) * 8; e += 64 * kWaves) {
-        const int have = left - (e & 7) * 16;
-        if (have < 16) {
-          i32x4* at = lds[half] + place(e >> 3, e & 7);
-          *at = first_bytes(*at, have);
-        }
+    else if (p.k & 15) {
+      // and in place of the bytes behind the row in its last chunk
+      for (int row = threadIdx.x; row < BM + BN; row += 64 * kWaves) {
+        i32x4* at = lds[half] + place(row, (p.k & (WDP_BLOCK - 1)) >> 4);
+        *at = first_bytes(*at, p.k & 15);
       }
       __syncthreads();
     }
