@@ -194,6 +194,23 @@ def wd_last_error(handle):
     return load_library().wd_last_error(handle).decode()
 
 
+def _verify_actions(envs, probs, draft_probs, u, draws, what):
+    """Actions that were sampled from draft_probs, made draws from probs in place (``wdp_verify``); True where one was kept."""
+    import torch
+
+    from .policy import verify_drafts
+
+    for name, t in (("probs", probs), ("draft_probs", draft_probs)):
+        if t.dtype != torch.float32 or not t.is_contiguous() or t.device != envs.device or t.numel() != envs.layout.probs_elems:
+            raise ValueError(f"{name} must be a contiguous float32 device tensor of shape {what}")
+    if u.dtype != torch.float32 or not u.is_contiguous() or u.device != envs.device or u.numel() != 2 * draws:
+        raise ValueError("u must be a contiguous float32 device tensor with two numbers for each action")
+    drafts = envs.action.view(draws, 1)
+    with torch.cuda.stream(envs.torch_stream):
+        accepted, _ = verify_drafts(probs.view(draws, 1, 5), draft_probs.view(draws, 1, 5), drafts, u.view(draws, 2), tokens=drafts)
+        return accepted.view(envs.action.shape).bool()
+
+
 # ---- convenience: buffers allocated by PyTorch on the device ------------------------------------
 class TagEnvs:
     """E Tag environments resident on one GPU.  PyTorch allocates the state tensors and supplies
@@ -234,6 +251,12 @@ class TagEnvs:
     def sample(self, probs):
         self._check_probs(probs)
         wd_sample(self.handle, probs.data_ptr())
+
+    def verify(self, probs, draft_probs, u):
+        """Between ``sample(draft_probs)`` and ``step()``: the actions that a cheaper or older policy drafted become draws
+        from ``probs`` ([E, N, 5], like draft_probs), as few of them as can be redrawn.  u: uniform numbers [E, N, 2], one
+        for the test and one for the new draw.  Returns which actions were kept ([E, N], bool)."""
+        return _verify_actions(self, probs, draft_probs, u, self.E * self.N, "[E, N, 5]")
 
     def step(self):
         wd_step(self.handle)
@@ -476,6 +499,10 @@ class CTagEnvs:
     def sample(self, probs):
         self._check_probs(probs)
         wdc_sample(self.handle, probs.data_ptr())
+
+    def verify(self, probs, draft_probs, u):
+        """``TagEnvs.verify`` for both actions of every agent: probs, draft_probs [E, N, 2, 5], u [E, N, 2, 2], result [E, N, 2]."""
+        return _verify_actions(self, probs, draft_probs, u, 2 * self.E * self.N, "[E, N, 2, 5]")
 
     def step(self):
         wdc_step(self.handle)

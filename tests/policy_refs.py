@@ -48,14 +48,17 @@ def norm_backward(dy, h, weight, rstd, dh):
 
 
 def product(a, a_scale, b, b_scale, by_row):
-    """(c, sum of the terms' sizes) in float64."""
+    """(c, sum of the terms' sizes, sum over the blocks of 128 * (largest a) * (largest b)) in float64."""
     def spread(scale, rows, n, k):
         s = f64(scale).repeat_interleave(BLOCK, 1)[:, :k]
         return s if rows == 1 else s.repeat_interleave(rows, 0)[:n]
 
+    def largest(v):
+        return torch.stack([x.abs().amax(1) for x in v.split(BLOCK, 1)], 1)
+
     (m, k), n = a.shape, b.shape[0]
     av, bv = a.cpu().float().double() * spread(a_scale, 1, m, k), b.cpu().float().double() * spread(b_scale, 1 if by_row else BLOCK, n, k)
-    return av @ bv.t(), av.abs() @ bv.abs().t()
+    return av @ bv.t(), av.abs() @ bv.abs().t(), BLOCK * largest(av) @ largest(bv).t()
 
 
 def verify(target, draft, drafts, u, lengths=None):
