@@ -340,6 +340,63 @@ def continuous_figures(cfg, steps=None, warmup=50):
             "algorithmic_bytes_per_iteration": nbytes, "hbm_frac": nbytes / (ev / steps) / 1e9 / HBM_PEAK_GBS}
 
 
+def policy_figures(cfg, width=256, steps=20):
+    """The workload with a policy in the loop (include/wdp.h): observations through norm and 8-bit products (two layers of
+    `width`, the second with a residual) to the probabilities of wd_iterate; the same with the policy's draws taken from a
+    cheaper one's drafts (sample, verify, step, reset); one step of the optimiser over the policy's weights.  us each."""
+    import torch
+    import paper_2108_13976_amd as wd
+
+    envs = wd.TagEnvs(**cfg.kwargs())
+    envs.reset(wd.WD_RESET_ALL)
+    E, N, D = envs.E, envs.N, envs.D
+    gen = torch.Generator(device="cuda:0").manual_seed(cfg.seed)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=gen, device="cuda:0")
+
+    weights = [normal(width, D) / D ** 0.5, normal(width, width) / width ** 0.5, normal(5, width) / width ** 0.5]
+    norms = [torch.ones(d, device="cuda:0") for d in (D, width, width)]
+    eight = [wd.quantise8(w) for w in weights]
+    e4m3 = torch.float8_e4m3fn
+
+    def policy():
+        x = wd.rms_norm(envs.obs.view(E * N, D), norms[0], out8=e4m3)
+        h = wd.product8(x.q, x.scale, *eight[0])
+        x = wd.rms_norm(h, norms[1], out8=e4m3)
+        x = wd.rms_norm(wd.product8(x.q, x.scale, *eight[1]), norms[2], residual=h, h=h, out8=e4m3)
+        return torch.softmax(wd.product8(x.q, x.scale, *eight[2], dtype=torch.float32), -1).view(E, N, 5)
+
+    params = weights + norms
+    grads = [0.01 * normal(*p.shape) for p in params]
+    optimiser = wd.AdamW(params, grads)
+    drafts = torch.softmax(normal(E, N, 5), -1)
+    u = torch.rand((E, N, 2), generator=gen, device="cuda:0")
+    probs = policy()
+
+    def drafted():
+        envs.sample(drafts)
+        envs.verify(probs, drafts, u)
+        envs.step()
+        envs.reset(wd.WD_RESET_DONE)
+
+    out = {"width": width}
+    for name, call in (("policy_us", policy), ("iterate_with_policy_us", lambda: envs.iterate(policy())), ("drafted_iteration_us", drafted),
+                       ("optimiser_step_us", optimiser.step)):
+        for _ in range(3):
+            call()
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        torch.cuda.synchronize()
+        start.record()
+        for _ in range(steps):
+            call()
+        end.record()
+        torch.cuda.synchronize()
+        out[name] = start.elapsed_time(end) / steps * 1e3
+    envs.close()
+    return out
+
+
 def time_continuous_oracle(cfg, envs, iterations, threads):
     import numpy as np
     from oracle import ctag_oracle, tag_oracle
@@ -597,6 +654,8 @@ def main():
             # continuous Tag (paper Sec. 5.1, second variant): its three workloads, 2 T iterations after 50
             from workloads import CTAG_CONFIGS
             extras["continuous_tag"] = {name: continuous_figures(c) for name, c in CTAG_CONFIGS.items()}
+            # the policy's operators on this workload's observations
+            extras["policy_in_the_loop"] = policy_figures(cfg)
         out["extras"] = extras
 
     if not args.no_cpu_baseline:

@@ -10,6 +10,7 @@ import paper_2108_13976_amd as wd
 from paper_2108_13976_amd import binding, policy
 
 import policy_refs as ref
+from test_kernel_resources import notes  # noqa: F401
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 NULL, CONFIG, ALIGN, UNSUPPORTED = binding.WD_E_NULL, binding.WD_E_CONFIG, binding.WD_E_ALIGN, binding.WD_E_UNSUPPORTED
@@ -293,3 +294,24 @@ def test_reference_gradients_against_differences():
         to = torch.randn(t.shape, generator=gen, dtype=torch.float64)
         up, down = (loss(x + s * to, w) if t is x else loss(x, w + s * to) for s in (1e-5, -1e-5))
         assert abs((up - down) / 2e-5 - (grad * to).sum()) < 1e-7
+
+
+# ---- the built kernels --------------------------------------------------------------------------
+def test_kernels_keep_their_state_in_registers(notes):  # noqa: F811
+    """But for rows of more than 8192 elements (1024 threads have 128 registers each) and the tiles of operands whose rows do not
+    start at 16-byte boundaries, exact ones."""
+    import subprocess
+
+    found = {}
+    for mangled, numbers in notes.items():
+        if "wdp" in mangled:
+            found[mangled] = numbers
+    names = subprocess.run(["c++filt"], input="\n".join(found), stdout=subprocess.PIPE, text=True, check=True).stdout.split("\n")
+    for mangled, name in zip(found, names):
+        wide = "norm_" in mangled and ("Li1024ELi2" in mangled or "Li1024ELi4" in mangled)
+        fallback = "product_tile_kernel" in mangled
+        if not (wide or fallback):
+            assert found[mangled]["private_segment_fixed_size"] == 0 and found[mangled]["vgpr_spill_count"] == 0, name
+    for part in ("norm_kernel", "norm_grad_kernel", "norm_grad_join_kernel", "product_tile_kernel", "product_large_kernel", "product_stream_kernel",
+                 "product_panel_kernel", "verify_lane_kernel", "verify_group_kernel", "verify_row_kernel", "verify_sums_kernel", "verify_find_kernel", "adamw_kernel"):
+        assert any(part in m for m in found), part
