@@ -14,6 +14,9 @@ namespace {
 constexpr int kVec = 8;          // elements of a lane's chunk
 constexpr int kMaxWidth = 32768; // 1024 threads x 4 chunks x 8
 
+// Threads of a workgroup whose rows have TPR lanes each: four waves of narrow rows, or one wide row.
+template <int TPR> constexpr int kThreadsOf = TPR <= 64 ? 256 : TPR;
+
 struct NormArgs {
   const void *x, *residual, *weight;
   void *h, *y;
@@ -51,7 +54,7 @@ template <int TPR> __device__ __forceinline__ float row_sum(float v, float (*pla
 }
 
 // Where a lane's chunk lies.  The chunk that the row ends in is moved back to end with it (rows of eight elements and
-// more): one access like the others, its first `skip` elements are its neighbour's.  (Elements one by one would cost every
+// more): one access like the others, its first `skip` elements are its neighbour's, which counts and writes them alone.  (Elements one by one would cost every
 // wave of an odd width a second pass of loads: 33333 x 999 bfloat16 took 97 us forward and 172 backward that way.)
 struct Span {
   int start, skip, count;  // count: elements that exist; 0: none
@@ -62,9 +65,29 @@ template <int TPR> __device__ __forceinline__ Span span_of(int width, int c) {
   if (left <= 0) return {0, kVec, 0};
   return width >= kVec ? Span{width - kVec, kVec - left, kVec} : Span{0, 0, left};
 }
-// A chunk as it lies in memory: requested one row ahead of its use, where the registers hold a row more (1024 threads have
-// 128 each).
-template <int TPR, int C> constexpr bool kAhead = TPR < 1024 || C == 1;
+// A chunk's own elements to memory (in place, the neighbour's may have been written by then).
+template <typename T> __device__ __forceinline__ void store_span(T* row, const Span& s, const float v[kVec]) {
+  T* p = row + s.start;
+  if (s.count == kVec && s.skip == 0) return store_vec<T, kVec>(p, v);
+  if constexpr (sizeof(T) == 2) {
+    uint64_t lo = uint64_t(narrow<T>(v[2], v[3])) << 32 | narrow<T>(v[0], v[1]), hi = uint64_t(narrow<T>(v[6], v[7])) << 32 | narrow<T>(v[4], v[5]);
+    const int by = 16 * (s.skip & 3), n = s.count - s.skip;
+    p += s.skip;
+    if (s.skip & 4) lo = hi, hi = 0;
+    if (by) lo = lo >> by | hi << (64 - by), hi >>= by;
+    if (n & 4) store_raw(p, lo), lo = hi, p += 4;
+    if (n & 2) store_raw(p, uint32_t(lo)), lo >>= 32, p += 2;
+    if (n & 1) store_raw(p, uint16_t(lo));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (i >= s.skip && i < s.count) p[i] = v[i];
+  }
+}
+
+// A chunk as it lies in memory: requested one row ahead of its use, where the registers hold a row more (768 threads and
+// more have 128 to 168 each).
+template <int TPR, int C> constexpr bool kAhead = TPR < 768 || C == 1;
 template <typename T> struct Words {
   u32x4 w[sizeof(T) / 2];
 };
@@ -84,12 +107,16 @@ template <typename T> __device__ __forceinline__ Words<T> request(const T* row, 
   }
   return r;
 }
-template <typename T> __device__ __forceinline__ void values(const Words<T>& r, float v[kVec]) {
+// Its values; with OWN those that are the neighbour's read as zero.
+template <bool OWN, typename T> __device__ __forceinline__ void values(const Words<T>& r, const Span& s, float v[kVec]) {
 #pragma unroll
   for (int i = 0; i < kVec; i += sizeof(T) == 4 ? 1 : 2) {
     if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(r.w[i / 4][i % 4]);
     else widen<T>(r.w[0][i / 2], v + i);
   }
+#pragma unroll
+  for (int i = 0; i < kVec; ++i)
+    if (OWN && i < s.skip) v[i] = 0.0f;
 }
 template <typename W> __device__ __forceinline__ void load_weight(const void* weight, const Span& s, float w[kVec]) {
   if (weight) {
@@ -101,12 +128,12 @@ template <typename W> __device__ __forceinline__ void load_weight(const void* we
 }
 
 template <typename T, typename W, int TPR, int C>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a) {
-  constexpr int kThreads = TPR > 256 ? TPR : 256, kRows = kThreads / TPR;
+__global__ __launch_bounds__(kThreadsOf<TPR>) void norm_kernel(NormArgs a) {
+  constexpr int kThreads = kThreadsOf<TPR>, kRows = kThreads / TPR;
   __shared__ float places[2][16];
   const int lane = threadIdx.x % TPR;
   int turn = 0;
-  float w[C][kVec];
+  float w[C > 2 ? 1 : C][kVec];
   Span at[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -131,27 +158,45 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
       if (residual) next_r[c] = request(residual + row * a.residual_stride, at[c]);
     }
   };
+  const auto store_row = [](T* row, const Span& s, const float v[kVec]) {
+    if (C > 2) store_span<T>(row, s, v);
+    else store_some<T, kVec>(row + s.start, s.count, v);
+  };
   int64_t row = int64_t(blockIdx.x) * run + threadIdx.x / TPR;
   if (kAhead<TPR, C> && row < a.rows) ahead(row);
   for (int64_t next; row < a.rows; row = next) {
     next = following(row);
-    if (!kAhead<TPR, C>) ahead(row);
-    float v[C][kVec];
+    if (!kAhead<TPR, C> && C <= 2) ahead(row);
+    float v[C > 2 ? 1 : C][kVec];
+    const auto sums = [&](int c, float v[kVec]) {  // of x and residual, as h is stored: the norm is that of h
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[i] = 0.0f;
+      if (!at[c].count) return;
+      values<(C > 2)>(next_x[c], at[c], v);
+      if (residual) {
+        float r[kVec];
+        values<(C > 2)>(next_r[c], at[c], r);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = to_float<T>(from_float<T>(v[i] + r[i]));
+      }
+    };
     float square = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) v[c][i] = 0.0f;
-      if (!at[c].count) continue;
-      values(next_x[c], v[c]);
-      if (residual) {
-        float r[kVec];
-        values(next_r[c], r);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[c][i] = to_float<T>(from_float<T>(v[c][i] + r[i]));  // the norm is that of h as it is stored
+      float* u = v[C > 2 ? 0 : c];
+      if (C > 2) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (at[c].count) {
+          next_x[c] = request(x + row * a.x_stride, at[c]);
+          if (residual) next_r[c] = request(residual + row * a.residual_stride, at[c]);
+        }
       }
+      sums(c, u);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) square = fmaf(i < at[c].skip ? 0.0f : v[c][i], v[c][i], square);
+      for (int i = 0; i < kVec; ++i) {
+        const float own = i < at[c].skip ? 0.0f : u[i];
+        square = fmaf(own, own, square);
+      }
     }
     if (kAhead<TPR, C> && next < a.rows) ahead(next);
     const float rstd = 1.0f / sqrtf(row_sum<TPR>(square, places, turn) * a.inv_width + a.eps);
@@ -159,17 +204,27 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
     if (a.rstd && lane == 0) a.rstd[row] = rstd;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      // (what a moved chunk writes of its neighbour's elements is what the neighbour writes)
-      if (at[c].count && a.h) store_some<T, kVec>(static_cast<T*>(a.h) + row * a.h_stride + at[c].start, at[c].count, v[c]);
-      if (C > 2 && at[c].count) load_weight<W>(a.weight, at[c], w[c]);
+      float* u = v[C > 2 ? 0 : c];
+      if (C > 2) {  // (the widest rows are read twice, the second time from the cache, a chunk at a time)
+        __builtin_amdgcn_sched_barrier(0);
+        if (at[c].count) {
+          next_x[c] = request(x + row * a.x_stride, at[c]);
+          if (residual) next_r[c] = request(residual + row * a.residual_stride, at[c]);
+          load_weight<W>(a.weight, at[c], w[0]);
+        }
+        sums(c, u);
+      }
+      // (a row held in registers was read whole before anything of it is written: there a moved chunk writes of its
+      // neighbour's elements what the neighbour writes, in one access)
+      if (at[c].count && a.h) store_row(static_cast<T*>(a.h) + row * a.h_stride, at[c], u);
       float y[kVec];
       float most = 0.0f;
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        y[i] = i < at[c].count ? v[c][i] * rstd * w[c][i] : 0.0f;
+        y[i] = i >= at[c].count ? 0.0f : u[i] * rstd * w[C > 2 ? 0 : c][i];
         most = fmaxf(most, i < at[c].skip ? 0.0f : fabsf(y[i]));
       }
-      if (at[c].count && a.y) store_some<T, kVec>(static_cast<T*>(a.y) + row * a.y_stride + at[c].start, at[c].count, y);
+      if (at[c].count && a.y) store_row(static_cast<T*>(a.y) + row * a.y_stride, at[c], y);
       if (a.q) {
         most = fmaxf(group_max<(TPR < 16 ? TPR : 16)>(most), kTiny);
         const float largest = a.q_type == WDP_E4M3 ? kLargestE4M3 : kLargestE5M2;
@@ -197,18 +252,19 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
 }
 
 template <typename T, typename W, int TPR, int C>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_grad_kernel(GradArgs a) {
-  constexpr int kThreads = TPR > 256 ? TPR : 256, kRows = kThreads / TPR;
+__global__ __launch_bounds__(kThreadsOf<TPR>) void norm_grad_kernel(GradArgs a) {
+  constexpr int kThreads = kThreadsOf<TPR>, kRows = kThreads / TPR;
   __shared__ float places[2][16];
   int turn = 0;
-  float w[C][kVec], dw[C][kVec];
+  constexpr bool kTwice = C > 2 || (C == 2 && TPR == 1024 && sizeof(T) == 4);  // the widest rows are read twice (and their weights with them), the second time from the cache
+  float w[kTwice ? 1 : C][kVec], dw[C][kVec];
   Span at[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     at[c] = span_of<TPR>(a.width, c);
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) w[c][i] = dw[c][i] = 0.0f;
-    if (at[c].count) load_weight<W>(a.weight, at[c], w[c]);
+    for (int i = 0; i < kVec; ++i) w[kTwice ? 0 : c][i] = dw[c][i] = 0.0f;
+    if (!kTwice && at[c].count) load_weight<W>(a.weight, at[c], w[c]);
   }
   const T *from_dy = static_cast<const T*>(a.dy), *from_h = static_cast<const T*>(a.h), *from_dh = static_cast<const T*>(a.dh);
   Words<T> next_dy[C], next_h[C], next_dh[C];
@@ -227,30 +283,43 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_grad_kernel(GradAr
   int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / TPR;
   if (kAhead<TPR, C> && row < a.rows) ahead(row);
   for (; row < a.rows; row += step) {
-    if (!kAhead<TPR, C>) ahead(row);
-    float dy[C][kVec], xhat[C][kVec];
+    if (!kAhead<TPR, C> && !kTwice) ahead(row);
+    const float rstd = kTwice ? a.rstd[row] : next_rstd;
+    float g[kTwice ? 1 : C][kVec], xhat[kTwice ? 1 : C][kVec];
     Words<T> dh[C];
+    const auto chunk = [&](int c, float g[kVec], float xhat[kVec]) {  // dy and h * rstd
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) g[i] = xhat[i] = 0.0f;
+      if (!at[c].count) return;
+      if (kTwice) {
+        next_dy[c] = request(from_dy + row * a.dy_stride, at[c]);
+        next_h[c] = request(from_h + row * a.h_stride, at[c]);
+        load_weight<W>(a.weight, at[c], w[0]);
+      }
+      values<true>(next_dy[c], at[c], g);
+      values<true>(next_h[c], at[c], xhat);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) xhat[i] *= rstd;
+    };
     float dot = 0.0f;
-    const float rstd = next_rstd;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) dy[c][i] = xhat[c][i] = 0.0f;
-      if (!at[c].count) continue;
-      values(next_dy[c], dy[c]);
-      values(next_h[c], xhat[c]);
-      if (kAhead<TPR, C> && from_dh) dh[c] = next_dh[c];
+    for (int c = 0; c < (kTwice ? 0 : C); ++c) {
+      chunk(c, g[c], xhat[c]);
+      if (kAhead<TPR, C> && from_dh && at[c].count) dh[c] = next_dh[c];
     }
     if (kAhead<TPR, C> && row + step < a.rows) ahead(row + step);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+      const int u = kTwice ? 0 : c;
+      if (kTwice) {
+        __builtin_amdgcn_sched_barrier(0);  // (a chunk at a time in the registers)
+        chunk(c, g[u], xhat[u]);
+      }
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        xhat[c][i] *= rstd;
-        const float g = i < at[c].skip ? 0.0f : dy[c][i];
-        dw[c][i] = fmaf(g, xhat[c][i], dw[c][i]);
-        dot = fmaf(g * w[c][i], xhat[c][i], dot);
-        dy[c][i] *= w[c][i];
+        dw[c][i] = fmaf(g[u][i], xhat[u][i], dw[c][i]);
+        g[u][i] *= w[u][i];
+        dot = fmaf(g[u][i], xhat[u][i], dot);
       }
     }
     if (!a.dx) continue;
@@ -258,17 +327,22 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_grad_kernel(GradAr
     turn ^= 1;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+      const int u = kTwice ? 0 : c;
+      if (kTwice) {
+        __builtin_amdgcn_sched_barrier(0);  // (a chunk at a time in the registers)
+        chunk(c, g[u], xhat[u]);
+      }
       if (!at[c].count) continue;
       float dx[kVec], more[kVec];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) more[i] = 0.0f;
       if (from_dh) {
         if (!kAhead<TPR, C>) dh[c] = request(from_dh + row * a.dh_stride, at[c]);
-        values(dh[c], more);
+        values<true>(dh[c], at[c], more);
       }
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) dx[i] = rstd * (dy[c][i] - xhat[c][i] * mean) + more[i];
-      store_some<T, kVec>(static_cast<T*>(a.dx) + row * a.dx_stride + at[c].start, at[c].count, dx);
+      for (int i = 0; i < kVec; ++i) dx[i] = rstd * ((kTwice ? g[u][i] * w[u][i] : g[u][i]) - xhat[u][i] * mean) + more[i];
+      store_span<T>(static_cast<T*>(a.dx) + row * a.dx_stride, at[c], dx);
     }
   }
   if (!a.partial) return;
@@ -324,13 +398,13 @@ __global__ __launch_bounds__(1024) void norm_grad_join_kernel(const float* __res
 int rows_a_block(int width) { return width <= 32 ? 64 : width <= 64 ? 32 : width <= 128 ? 16 : width <= 256 ? 8 : width <= 1024 ? 4 : 1; }
 
 int64_t grad_blocks(const wdp_norm_config& c) {
-  const int64_t per = rows_a_block(c.width), all = (c.rows + per - 1) / per, most = c.width > 4096 ? 256 : 1024;
+  const int64_t per = rows_a_block(c.width), all = (c.rows + per - 1) / per, most = c.width > 4096 ? 256 : c.width > 2048 ? 512 : 1024;
   return all < most ? all : most;
 }
 
 template <typename T, typename W> struct Norm {
   template <int TPR, int C> static void run(NormArgs a, hipStream_t stream) {
-    constexpr int threads = TPR > 256 ? TPR : 256, per = threads / TPR;
+    constexpr int threads = kThreadsOf<TPR>, per = threads / TPR;
     const int64_t most = 2048 * 256 / threads;
     a.run = per < 32 && TPR <= 64 && a.rows > 32 * most ? 32 : per;  // (few rows: one round of as many workgroups as there can be)
     const int64_t all = (a.rows + a.run - 1) / a.run;
@@ -339,7 +413,7 @@ template <typename T, typename W> struct Norm {
 };
 template <typename T, typename W> struct Grad {
   template <int TPR, int C> static void run(const GradArgs& a, unsigned blocks, hipStream_t stream) {
-    norm_grad_kernel<T, W, TPR, C><<<dim3(blocks), dim3(TPR > 256 ? TPR : 256), 0, stream>>>(a);
+    norm_grad_kernel<T, W, TPR, C><<<dim3(blocks), dim3(kThreadsOf<TPR>), 0, stream>>>(a);
   }
 };
 
@@ -351,9 +425,13 @@ template <template <typename, typename> class K, typename T, typename W, typenam
   else if (width <= 256) K<T, W>::template run<32, 1>(args...);
   else if (width <= 512) K<T, W>::template run<64, 1>(args...);
   else if (width <= 1024) K<T, W>::template run<64, 2>(args...);
+  else if (width <= 1536) K<T, W>::template run<192, 1>(args...);
   else if (width <= 2048) K<T, W>::template run<256, 1>(args...);
-  else if (width <= 4096) K<T, W>::template run<256, 2>(args...);
+  else if (width <= 2560) K<T, W>::template run<320, 1>(args...);
+  else if (width <= 4096) K<T, W>::template run<512, 1>(args...);
+  else if (width <= 6144) K<T, W>::template run<768, 1>(args...);
   else if (width <= 8192) K<T, W>::template run<1024, 1>(args...);
+  else if (width <= 12288) K<T, W>::template run<768, 2>(args...);
   else if (width <= 16384) K<T, W>::template run<1024, 2>(args...);
   else K<T, W>::template run<1024, 4>(args...);
 }

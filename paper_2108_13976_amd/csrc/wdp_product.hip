@@ -95,12 +95,9 @@ __device__ __forceinline__ i32x4 first_bytes(i32x4 v, int have) {
 // Sixteen bytes of a row at `at`; those from `left` on do not exist and read as zero.  A chunk at a 16-byte boundary that
 // holds a byte of the row can be read whole (no page ends inside it).
 __device__ __forceinline__ i32x4 load_chunk(const uint8_t* row, int64_t at, int left, bool aligned) {
-  struct __attribute__((packed, aligned(1))) Raw {
-    i32x4 v;
-  };
-  if (left >= 16) return reinterpret_cast<const Raw*>(row + at)->v;
+  if (left >= 16) return load_raw<i32x4>(row + at);
   if (left <= 0) return i32x4{0, 0, 0, 0};
-  if (aligned) return first_bytes(reinterpret_cast<const Raw*>(row + at)->v, left);
+  if (aligned) return first_bytes(load_raw<i32x4>(row + at), left);
   uint64_t lo = 0, hi = 0;
 #pragma unroll 1
   for (int i = 0; i < left; ++i) {
@@ -471,9 +468,6 @@ __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs 
       bs[j][e] = p.b_scale + int64_t(p.by_row ? at : at / WDP_BLOCK) * p.bs_row;
     }
   }
-  struct __attribute__((packed, aligned(1))) Raw {
-    i32x4 v;
-  };
   i32x4 la[DEPTH][TM][2], lb[DEPTH][TN][2];
   float sa[DEPTH][TM], sb[DEPTH][TN][4];
   auto scales = [&](int d, int block) {
@@ -508,9 +502,9 @@ __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs 
     for (int d = 0; d < DEPTH; ++d) {
       const int64_t k0 = int64_t(block + d * WAVES) * WDP_BLOCK;
 #pragma unroll
-      for (int j = 0; j < TN; ++j) lb[d][j][0] = reinterpret_cast<const Raw*>(b[j] + k0)->v, lb[d][j][1] = reinterpret_cast<const Raw*>(b[j] + k0 + 64)->v;
+      for (int j = 0; j < TN; ++j) lb[d][j][0] = load_raw<i32x4>(b[j] + k0), lb[d][j][1] = load_raw<i32x4>(b[j] + k0 + 64);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) la[d][i][0] = reinterpret_cast<const Raw*>(a[i] + k0)->v, la[d][i][1] = reinterpret_cast<const Raw*>(a[i] + k0 + 64)->v;
+      for (int i = 0; i < TM; ++i) la[d][i][0] = load_raw<i32x4>(a[i] + k0), la[d][i][1] = load_raw<i32x4>(a[i] + k0 + 64);
       scales(d, block + d * WAVES);
     }
 #pragma unroll
@@ -646,9 +640,10 @@ template <int FA, int FB, typename C, int PN, int KB> void launch_panel(ProductA
 //   - Many rows against up to 64 columns and 256 of k: b in LDS.  2000000 x 5 x 64: 38 against 108 in tiles of 64;
 //     300000 x 47 x 200: 26 against 28; 10000 x 5 x 300 would take 8.7 against 5.2, hence the bound on m.
 //   - Up to 128 tiles of 64 x 64 (a launch of tiles would leave half the chip idle through all of k): b streamed, in the
-//     largest piece of c that still makes 240 workgroups.  128 x 4096 x 4096: 15 against 20; 700 x 700 x 3000: 10 against 16;
-//     beyond, 200 x 4096 x 4096: 28 against 21.  With k of one or two blocks there is nothing to stream: 2000 x 256 x 128
-//     takes 4.0 against 3.2, so only up to 32 tiles there (300 x 200 x 256: 2.8 against 3.6).
+//     largest piece of c, not above m rows, that still makes 150 workgroups (a CU brings some 27 GB/s, so it takes many).
+//     128 x 4096 x 4096: 15 against 20; 700 x 700 x 3000: 10 against 16; 112 x 2445 x 5638: 16 in pieces of 64 x 32, 22 in
+//     32 x 32, 24 in tiles; beyond, 200 x 4096 x 4096: 28 against 21.  With k of one or two blocks there is nothing to stream:
+//     2000 x 256 x 128 takes 4.0 against 3.2, so only up to 32 tiles there (300 x 200 x 256: 2.8 against 3.6).
 //   - Rows that do not start at 16-byte boundaries: tiles by way of registers.
 //   - Else the tiles that need the least time for a block of k: rounds of 256 tiles of 256 x 256 at 2.1, 512 of 128 x 128
 //     at 1.2 (1.0 with one tile a CU at most), 1024 of 64 x 64 at 1.5 (0.95, 0.65 with two, one a CU); exact ones 2.0 and
@@ -664,9 +659,9 @@ template <int FA, int FB, typename C> void launch_slice(const ProductArgs& p, hi
     return launch_panel<FA, FB, C, 64, 2>(p, stream);
   }
   if (t64 <= 128 && (p.blocks > 2 || t64 <= 32)) {
-    if (tiles(64, 32) >= 240) return launch_stream<FA, FB, C, 4, 2, 8, 1>(p, stream);
-    if (tiles(32, 32) >= 240) return launch_stream<FA, FB, C, 2, 2, 8, 2>(p, stream);
-    if (tiles(32, 16) >= 240) return launch_stream<FA, FB, C, 2, 1, 8, 2>(p, stream);
+    if (p.m > 32 && tiles(64, 32) >= 150) return launch_stream<FA, FB, C, 4, 2, 8, 1>(p, stream);
+    if (p.m > 16 && tiles(32, 32) >= 150) return launch_stream<FA, FB, C, 2, 2, 8, 2>(p, stream);
+    if (p.m > 16 && tiles(32, 16) >= 150) return launch_stream<FA, FB, C, 2, 1, 8, 2>(p, stream);
     return launch_stream<FA, FB, C, 1, 1, 8, 4>(p, stream);
   }
   // (places in a tile are 32-bit offsets from its first row)

@@ -775,3 +775,35 @@ def test_gradients_of_the_8_bit_product_by_the_product_itself():
     for got, want, terms in ((da, ref.f64(dc) @ ref.f64(b), ref.f64(dc).abs() @ ref.f64(b).abs()),
                              (db, ref.f64(dc).t() @ ref.f64(a), ref.f64(dc).abs().t() @ ref.f64(a).abs())):
         assert ((ref.f64(got) - want).abs() <= ((1 + 2.0 ** -3) * (1 + 2.0 ** -4) - 1 + 1e-3) * terms).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [9, 21, 300, 999, 1100, 3001, 4797, 9001, 12001, 16001, 20001])
+def test_norm_and_its_gradients_in_place_where_the_row_ends_inside_a_chunk(width, dtype):
+    """The row's last chunk overlaps its neighbour's in memory: h over residual, dx over dh and over dy, many rows, twice the same
+    as out of place; a value that is not finite among the overlapped ones stays where it is."""
+    gen = generator(width, 51)
+    rows = 600 if width < 5000 else 300
+    x, r, dy, dh = (normal(gen, rows, width, dtype=dtype) for _ in range(4))
+    w = 1 + 0.1 * normal(gen, width)
+    x[1, width - 3], x[2, max(0, width - 9)] = float("inf"), float("inf")
+    want = wd.rms_norm(x, w, residual=r, out8=E4M3, y=True)
+    bad = torch.zeros(width, dtype=torch.bool, device=DEV)
+    for row, col in ((1, width - 3), (2, max(0, width - 9))):
+        bad.zero_()
+        bad[col] = True
+        assert torch.equal(want.y[row].isnan(), bad) and (want.y[row][~bad] == 0).all()
+    h = r.clone()
+    got = wd.rms_norm(x, w, residual=h, h=h, out8=E4M3, y=True)
+    for a, b in zip(want, got):
+        assert torch.equal(a.view(torch.uint8) if a.dtype == E4M3 else torch.nan_to_num(a, nan=7.0), b.view(torch.uint8) if b.dtype == E4M3 else torch.nan_to_num(b, nan=7.0))
+    h, rstd = torch.nan_to_num(want.h, posinf=0.5), torch.rsqrt(want.h.float().square().mean(1) + 1e-5)
+    dx, dw = wd.rms_norm_backward(dy, h, w, rstd, dh=dh)
+    cfg = raw_norm(rows, width, policy.WDP_BF16 if dtype == BF16 else policy.WDP_F32)
+    space = torch.empty(wd.wdp_norm_backward_workspace(cfg), dtype=torch.uint8, device=DEV)
+    for over_dy in (False, True):
+        first, second, dw2 = dy.clone(), dh.clone(), torch.empty_like(dw)
+        to = first if over_dy else second
+        wd.wdp_norm_backward(cfg, policy.wdp_norm_grad_buffers(first.data_ptr(), second.data_ptr(), h.data_ptr(), w.data_ptr(), rstd.data_ptr(), to.data_ptr(),
+                                                               dw2.data_ptr(), space.data_ptr()))
+        assert torch.equal(to, dx) and torch.equal(dw2, dw), over_dy
