@@ -6,7 +6,8 @@
 // the row's sum, so that the kernels below, which sum in different orders, answer alike.
 //
 // Forms by the vocabulary.  Few actions (a policy of Tag has five): a lane a sequence, the row in its registers.  Up to
-// 1024: sixteen lanes or a wave a sequence, no barrier.  Up to 4096: a workgroup.  Longer rows: a wave a piece of 1024
+// 1024: sixteen lanes (256) or a wave a sequence, no barrier (50000 x 2 x 100: 24 us with a wave each, 13 with sixteen
+// lanes).  Up to 4096: a workgroup.  Longer rows: a wave a piece of 1024
 // elements sums it, a second launch finds the piece that holds the drawn token and goes through that one alone.  Memory
 // bounds the large batches, the chain of dependent loads (drafts, their elements, the row, the token) the small ones.
 #include "wdp_common.h"
@@ -387,7 +388,8 @@ template <typename T> void launch(VerifyArgs a, hipStream_t stream) {
     if (a.vocab <= 8 && a.drafts == 1 && !a.bonus) verify_lane_kernel<T, 8, true><<<blocks(256), 256, 0, stream>>>(a);
     else if (a.vocab <= 8) verify_lane_kernel<T, 8, false><<<blocks(256), 256, 0, stream>>>(a);
     else if (a.vocab <= 64) verify_group_kernel<T, 16, 4><<<blocks(16), 256, 0, stream>>>(a);
-    else if (a.vocab <= 256) verify_group_kernel<T, 64, 4><<<blocks(4), 256, 0, stream>>>(a);
+    else if (a.vocab <= 128) verify_group_kernel<T, 16, 8><<<blocks(16), 256, 0, stream>>>(a);
+    else if (a.vocab <= 256) verify_group_kernel<T, 16, 16><<<blocks(16), 256, 0, stream>>>(a);
     else if (a.vocab <= 1024) verify_group_kernel<T, 64, 16><<<blocks(4), 256, 0, stream>>>(a);
     else if (a.vocab <= kRow) verify_row_kernel<T, 4><<<dim3(count), 256, 0, stream>>>(a);
     else {

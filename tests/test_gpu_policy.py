@@ -315,7 +315,7 @@ def check_verify(p, q, x, u, lengths=None, **how):
     return accepted, tokens
 
 
-VERIFY = [(1, 1, 1), (700, 1, 5), (257, 3, 5), (64, 8, 2), (33, 2, 16), (40, 4, 17), (21, 1, 100), (9, 3, 1000), (5, 64, 64), (12, 2, 1023), (12, 2, 1024), (7, 3, 1025),
+VERIFY = [(1, 1, 1), (700, 1, 5), (257, 3, 5), (64, 8, 2), (33, 2, 16), (40, 4, 17), (21, 1, 100), (9, 3, 1000), (5, 64, 64), (30, 3, 128), (30, 3, 129), (30, 2, 255), (30, 2, 256), (12, 2, 257), (40, 20, 65), (12, 2, 1023), (12, 2, 1024), (7, 3, 1025),
           (6, 4, 4095), (6, 4, 4096), (5, 3, 4097), (4, 2, 8192), (3, 5, 9999), (2, 1, 50000), (1, 2, 131073)]
 
 
