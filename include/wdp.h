@@ -76,7 +76,8 @@ typedef struct wdp_norm_config {
   float eps;              /* >= 0, finite                                                  */
   int64_t x_stride, residual_stride, h_stride, y_stride;
   int64_t q_stride;
-  int64_t scale_row_stride, scale_block_stride; /* scale of row m, block b at m * row + b * block */
+  int64_t scale_row_stride, scale_block_stride; /* scale of row m, block b at m * row + b * block
+                             (places of their own: strides >= 1 where there are several)   */
   int64_t dy_stride, dh_stride, dx_stride;      /* backward only                           */
   void* stream;
 } wdp_norm_config;
@@ -213,7 +214,8 @@ int wdp_verify(const wdp_verify_config* cfg, const wdp_verify_buffers* bufs);
  * (m) or high (s) 16 bits / 65536 of word e mod 4 of the random block of (seed; e / 4, step,
  * stream 4), where e numbers the elements of the call: 128 * (blocks of the tensors before)
  * + the place in the tensor.  A root above zero does not become zero.
- * A NaN or an infinity in a gradient reaches its element, with 8 bits also its block. */
+ * A NaN or an infinity in a gradient reaches its element, an infinity with 8 bits also its block.
+ * Tensors of a call do not overlap (each is updated once). */
 typedef struct wdp_adamw_config {
   uint32_t struct_size;      /* = sizeof(wdp_adamw_config)                                   */
   int32_t state_bits;        /* 32 or 8                                                      */

@@ -1,7 +1,8 @@
 // wdp_adamw.hip — one AdamW step over many tensors at once, states in 32 or 8 bits (include/wdp.h: wdp_adamw).
 //
 // The step reads and writes every weight and both states once and computes about twenty operations an element on the
-// way: memory bounds it, and for a small policy the launches do.  So the tensors travel in the kernel's arguments (48
+// way: memory bounds it (63 M weights of 2999 tensors, bfloat16 with 8-bit states: 204 us, 5.0 TB/s; 32-bit
+// states: 5.3 TB/s), and for a small policy the launches do (two tensors of 64: 4.8 us).  So the tensors travel in the kernel's arguments (48
 // at a time: nothing to copy to the device before the launch, nothing to keep alive behind it, and a captured step
 // holds its own), and a workgroup finds its tensor with one compare a lane over the tensors' first pieces.
 #include "wdp_common.h"
@@ -190,16 +191,15 @@ template <typename P, typename G, bool EIGHT> __global__ __launch_bounds__(kThre
   }
 }
 
-template <typename P, typename G> void launch_types(const AdamArgs& a, bool eight, unsigned blocks, hipStream_t stream) {
-  if (eight) adamw_kernel<P, G, true><<<dim3(blocks), dim3(kThreads), 0, stream>>>(a);
-  else adamw_kernel<P, G, false><<<dim3(blocks), dim3(kThreads), 0, stream>>>(a);
+template <typename P, typename G> int launch_types(const AdamArgs& a, bool eight, unsigned blocks, hipStream_t stream) {
+  return enqueue(eight ? adamw_kernel<P, G, true> : adamw_kernel<P, G, false>, dim3(blocks), kThreads, stream, a);
 }
-void launch(int param, int grad, const AdamArgs& a, bool eight, unsigned blocks, hipStream_t stream) {
-  if (param == WDP_F32) launch_types<float, float>(a, eight, blocks, stream);
-  else if (param == WDP_BF16 && grad == WDP_F32) launch_types<bf16, float>(a, eight, blocks, stream);
-  else if (param == WDP_BF16) launch_types<bf16, bf16>(a, eight, blocks, stream);
-  else if (grad == WDP_F32) launch_types<f16, float>(a, eight, blocks, stream);
-  else launch_types<f16, f16>(a, eight, blocks, stream);
+int launch(int param, int grad, const AdamArgs& a, bool eight, unsigned blocks, hipStream_t stream) {
+  if (param == WDP_F32) return launch_types<float, float>(a, eight, blocks, stream);
+  else if (param == WDP_BF16 && grad == WDP_F32) return launch_types<bf16, float>(a, eight, blocks, stream);
+  else if (param == WDP_BF16) return launch_types<bf16, bf16>(a, eight, blocks, stream);
+  else if (grad == WDP_F32) return launch_types<f16, float>(a, eight, blocks, stream);
+  return launch_types<f16, f16>(a, eight, blocks, stream);
 }
 
 bool amount(double v) { return v >= 0.0 && isfinite(v); }
@@ -244,27 +244,37 @@ extern "C" int wdp_adamw(const wdp_adamw_config* cfg, const wdp_adamw_tensor* te
     a.c2 = float(sqrt(1.0 / (1.0 - pow(cfg->beta2, double(cfg->step)))));
   }
   a.seed_lo = uint32_t(cfg->seed), a.seed_hi = uint32_t(cfg->seed >> 32);
-  // launches of up to 48 neighbouring tensors of the same types
+  // Launches of up to 48 neighbouring tensors of the same types, or pieces of them: a launch has fewer than 2^32 threads.
+  constexpr int64_t kMost = int64_t(1) << 23;  // workgroups of a launch
   uint32_t number = 0;
+  int64_t at = 0;  // elements of tensor i that are through
   for (int i = 0; i < count;) {
     const int param = tensors[i].param_type, grad = tensors[i].grad_type;
-    uint64_t blocks = 0;
+    int64_t blocks = 0;
     a.count = 0;
-    for (; i < count && a.count < kMaxTensors; ++i) {
+    while (i < count && a.count < kMaxTensors && blocks < kMost) {
       const wdp_adamw_tensor& t = tensors[i];
-      if (t.numel == 0) continue;
-      const uint64_t more = uint64_t((t.numel + kPiece - 1) / kPiece);
-      if (t.param_type != param || t.grad_type != grad || blocks + more > 0x7FFFFFFFu) break;
-      a.t[a.count] = Tensor{t.param, t.grad, t.master, t.exp_avg, t.exp_avg_sq, t.avg_scale, t.sq_scale, t.numel};
+      if (t.numel == 0) {
+        ++i;
+        continue;
+      }
+      if (t.param_type != param || t.grad_type != grad) break;
+      const int64_t left = t.numel - at, most = (kMost - blocks) * kPiece, n = left < most ? left : most;
+      const int64_t e = int64_t(size_of(t.param_type)), s = eight ? 1 : 4, scales = at / WDP_BLOCK * 4;
+      const auto moved = [](const void* p, int64_t bytes) { return p ? const_cast<char*>(static_cast<const char*>(p)) + bytes : nullptr; };
+      a.t[a.count] = Tensor{moved(t.param, at * e), moved(t.grad, at * int64_t(size_of(t.grad_type))), reinterpret_cast<float*>(moved(t.master, at * 4)),
+                            moved(t.exp_avg, at * s), moved(t.exp_avg_sq, at * s), reinterpret_cast<float*>(moved(t.avg_scale, scales)),
+                            reinterpret_cast<float*>(moved(t.sq_scale, scales)), n};
       a.first[a.count] = uint32_t(blocks);
       a.number[a.count] = number;
-      number += uint32_t((t.numel + WDP_BLOCK - 1) / WDP_BLOCK);
-      blocks += more;
+      number += uint32_t((n + WDP_BLOCK - 1) / WDP_BLOCK);
+      blocks += (n + kPiece - 1) / kPiece;
       ++a.count;
+      at += n;
+      if (at == t.numel) at = 0, ++i;
     }
     if (blocks == 0) continue;
-    launch(param, grad, a, eight, unsigned(blocks), static_cast<hipStream_t>(cfg->stream));
-    const int status = launched();
+    const int status = launch(param, grad, a, eight, unsigned(blocks), static_cast<hipStream_t>(cfg->stream));
     if (status != WD_OK) return status;
   }
   return WD_OK;

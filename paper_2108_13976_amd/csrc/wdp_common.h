@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "../../include/wdp.h"
 
@@ -22,10 +23,10 @@ inline int size_of(int type) { return type == WDP_F32 ? 4 : type == WDP_BF16 || 
 inline bool is_float_type(int type) { return type == WDP_F32 || type == WDP_BF16 || type == WDP_F16; }
 inline bool is_8bit(int type) { return type == WDP_E4M3 || type == WDP_E5M2; }
 
-// A launch that failed leaves nothing behind in the runtime's error state.
-inline int launched() {
-  const hipError_t err = hipGetLastError();
-  return err == hipSuccess ? WD_OK : WD_E_HIP;
+// One launch.  Its status is the launch's own: hipGetLastError would answer with what any earlier call of the program left.
+template <typename... P> int enqueue(void (*kernel)(P...), dim3 grid, int threads, hipStream_t stream, std::common_type_t<P>... args) {
+  void* list[] = {&args...};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(unsigned(threads)), list, 0, stream) == hipSuccess ? WD_OK : WD_E_HIP;
 }
 
 template <typename T> __device__ __forceinline__ float to_float(T v) { return static_cast<float>(v); }

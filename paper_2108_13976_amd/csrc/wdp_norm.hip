@@ -2,7 +2,8 @@
 // (include/wdp.h: wdp_norm, wdp_norm_backward).
 //
 // Both directions move each element once and compute a handful of operations on it: memory bounds them, latency where
-// there are few rows.  A row is held in registers by THREADS_PER_ROW lanes, eight adjacent elements a lane and chunk
+// there are few rows (2000000 x 256 bfloat16 with residual, sum and codes: 736 us, 4.9 TB/s, a copy's rate; 33333 x 999
+// backward: 57 us and 5 for the join; 50 x 256: 3.8 us on the device).  A row is held in registers by THREADS_PER_ROW lanes, eight adjacent elements a lane and chunk
 // (one 16-byte access of bfloat16), so that its mean square (or the gradient's inner product) is known before anything
 // is written and nothing is read twice.  Eight elements a lane make sixteen lanes a block of 128, whose maximum is
 // found by four exchanges within a row of sixteen lanes.
@@ -54,8 +55,9 @@ template <int TPR> __device__ __forceinline__ float row_sum(float v, float (*pla
 }
 
 // Where a lane's chunk lies.  The chunk that the row ends in is moved back to end with it (rows of eight elements and
-// more): one access like the others, its first `skip` elements are its neighbour's, which counts and writes them alone.  (Elements one by one would cost every
-// wave of an odd width a second pass of loads: 33333 x 999 bfloat16 took 97 us forward and 172 backward that way.)
+// more): one access like the others, its first `skip` elements are its
+// neighbour's, which counts and writes them alone.  (Elements one by one would cost every wave of an odd width a second
+// pass of loads: 33333 x 999 bfloat16 took 97 us forward and 172 backward that way.)
 struct Span {
   int start, skip, count;  // count: elements that exist; 0: none
 };
@@ -142,7 +144,7 @@ __global__ __launch_bounds__(kThreadsOf<TPR>) void norm_kernel(NormArgs a) {
   }
   // A workgroup takes runs of 32 neighbouring rows (a whole line of scales and of rstd, four bytes a row) in turn with the
   // others, which together go through memory from front to back: runs of a thousand rows each took 509 us for
-  // 2000000 x 256 without residual, single rounds of eight 940 with residual and scales, where runs of 32 take 428 and 767.
+  // 2000000 x 256 without residual, single rounds of eight 940 with residual and scales, where runs of 32 take 428 and 736.
   const int run = a.run;
   const auto following = [&](int64_t row) {
     const int64_t next = row + kRows;
@@ -403,44 +405,44 @@ int64_t grad_blocks(const wdp_norm_config& c) {
 }
 
 template <typename T, typename W> struct Norm {
-  template <int TPR, int C> static void run(NormArgs a, hipStream_t stream) {
+  template <int TPR, int C> static int run(NormArgs a, hipStream_t stream) {
     constexpr int threads = kThreadsOf<TPR>, per = threads / TPR;
     const int64_t most = 2048 * 256 / threads;
     a.run = per < 32 && TPR <= 64 && a.rows > 32 * most ? 32 : per;  // (few rows: one round of as many workgroups as there can be)
     const int64_t all = (a.rows + a.run - 1) / a.run;
-    norm_kernel<T, W, TPR, C><<<dim3(unsigned(all < most ? all : most)), dim3(threads), 0, stream>>>(a);
+    return enqueue(norm_kernel<T, W, TPR, C>, dim3(unsigned(all < most ? all : most)), threads, stream, a);
   }
 };
 template <typename T, typename W> struct Grad {
-  template <int TPR, int C> static void run(const GradArgs& a, unsigned blocks, hipStream_t stream) {
-    norm_grad_kernel<T, W, TPR, C><<<dim3(blocks), dim3(kThreadsOf<TPR>), 0, stream>>>(a);
+  template <int TPR, int C> static int run(const GradArgs& a, unsigned blocks, hipStream_t stream) {
+    return enqueue(norm_grad_kernel<T, W, TPR, C>, dim3(blocks), kThreadsOf<TPR>, stream, a);
   }
 };
 
 // Lanes a row by its width: as many as hold it with eight elements each, within a wave up to 1024 elements (no barrier).
-template <template <typename, typename> class K, typename T, typename W, typename... Args> void by_width(int width, Args... args) {
-  if (width <= 32) K<T, W>::template run<4, 1>(args...);
-  else if (width <= 64) K<T, W>::template run<8, 1>(args...);
-  else if (width <= 128) K<T, W>::template run<16, 1>(args...);
-  else if (width <= 256) K<T, W>::template run<32, 1>(args...);
-  else if (width <= 512) K<T, W>::template run<64, 1>(args...);
-  else if (width <= 1024) K<T, W>::template run<64, 2>(args...);
-  else if (width <= 1536) K<T, W>::template run<192, 1>(args...);
-  else if (width <= 2048) K<T, W>::template run<256, 1>(args...);
-  else if (width <= 2560) K<T, W>::template run<320, 1>(args...);
-  else if (width <= 4096) K<T, W>::template run<512, 1>(args...);
-  else if (width <= 6144) K<T, W>::template run<768, 1>(args...);
-  else if (width <= 8192) K<T, W>::template run<1024, 1>(args...);
-  else if (width <= 12288) K<T, W>::template run<768, 2>(args...);
-  else if (width <= 16384) K<T, W>::template run<1024, 2>(args...);
-  else K<T, W>::template run<1024, 4>(args...);
+template <template <typename, typename> class K, typename T, typename W, typename... Args> int by_width(int width, Args... args) {
+  if (width <= 32) return K<T, W>::template run<4, 1>(args...);
+  if (width <= 64) return K<T, W>::template run<8, 1>(args...);
+  if (width <= 128) return K<T, W>::template run<16, 1>(args...);
+  if (width <= 256) return K<T, W>::template run<32, 1>(args...);
+  if (width <= 512) return K<T, W>::template run<64, 1>(args...);
+  if (width <= 1024) return K<T, W>::template run<64, 2>(args...);
+  if (width <= 1536) return K<T, W>::template run<192, 1>(args...);
+  if (width <= 2048) return K<T, W>::template run<256, 1>(args...);
+  if (width <= 2560) return K<T, W>::template run<320, 1>(args...);
+  if (width <= 4096) return K<T, W>::template run<512, 1>(args...);
+  if (width <= 6144) return K<T, W>::template run<768, 1>(args...);
+  if (width <= 8192) return K<T, W>::template run<1024, 1>(args...);
+  if (width <= 12288) return K<T, W>::template run<768, 2>(args...);
+  if (width <= 16384) return K<T, W>::template run<1024, 2>(args...);
+  return K<T, W>::template run<1024, 4>(args...);
 }
-template <template <typename, typename> class K, typename... Args> void by_type(int type, int weight_type, int width, Args... args) {
-  if (type == WDP_F32) by_width<K, float, float>(width, args...);
-  else if (type == WDP_BF16 && weight_type == WDP_F32) by_width<K, bf16, float>(width, args...);
-  else if (type == WDP_BF16) by_width<K, bf16, bf16>(width, args...);
-  else if (weight_type == WDP_F32) by_width<K, f16, float>(width, args...);
-  else by_width<K, f16, f16>(width, args...);
+template <template <typename, typename> class K, typename... Args> int by_type(int type, int weight_type, int width, Args... args) {
+  if (type == WDP_F32) return by_width<K, float, float>(width, args...);
+  if (type == WDP_BF16 && weight_type == WDP_F32) return by_width<K, bf16, float>(width, args...);
+  if (type == WDP_BF16) return by_width<K, bf16, bf16>(width, args...);
+  if (weight_type == WDP_F32) return by_width<K, f16, float>(width, args...);
+  return by_width<K, f16, f16>(width, args...);
 }
 
 int check(const wdp_norm_config& c) {
@@ -469,7 +471,7 @@ int wdp_norm(const wdp_norm_config* cfg, const wdp_norm_buffers* b) {
   if (!stride_ok(*cfg, cfg->x_stride) || (b->residual && !stride_ok(*cfg, cfg->residual_stride)) || (b->h && !stride_ok(*cfg, cfg->h_stride)) ||
       (b->y && !stride_ok(*cfg, cfg->y_stride)) || (b->q && !stride_ok(*cfg, cfg->q_stride)))
     return WD_E_CONFIG;
-  if (b->q && (cfg->scale_row_stride < 0 || cfg->scale_block_stride < 0)) return WD_E_CONFIG;
+  if (b->q && (cfg->scale_row_stride < (cfg->rows > 1) || cfg->scale_block_stride < (cfg->width > WDP_BLOCK))) return WD_E_CONFIG;
   if (cfg->rows > 1 && ((b->h && b->h == b->x && cfg->h_stride != cfg->x_stride) || (b->h && b->h == b->residual && cfg->h_stride != cfg->residual_stride)))
     return WD_E_CONFIG;
   const size_t e = size_of(cfg->type);
@@ -479,8 +481,7 @@ int wdp_norm(const wdp_norm_config* cfg, const wdp_norm_buffers* b) {
   const NormArgs a = {b->x, b->residual, b->weight, b->h, b->y, static_cast<uint8_t*>(b->q), b->scale, b->rstd, cfg->rows, cfg->x_stride,
                       cfg->residual_stride, cfg->h_stride, cfg->y_stride, cfg->q_stride, cfg->scale_row_stride, cfg->scale_block_stride,
                       cfg->width, cfg->q_type, 0, cfg->eps, float(1.0 / cfg->width)};
-  by_type<Norm>(cfg->type, cfg->weight_type, cfg->width, a, static_cast<hipStream_t>(cfg->stream));
-  return launched();
+  return by_type<Norm>(cfg->type, cfg->weight_type, cfg->width, a, static_cast<hipStream_t>(cfg->stream));
 }
 
 int wdp_norm_backward_workspace(const wdp_norm_config* cfg, size_t* bytes) {
@@ -507,23 +508,21 @@ int wdp_norm_backward(const wdp_norm_config* cfg, const wdp_norm_grad_buffers* b
       return WD_E_CONFIG;
     const size_t e = size_of(cfg->type);
     if (!aligned(b->dy, e) || !aligned(b->dh, e) || !aligned(b->h, e) || !aligned(b->dx, e) || !aligned(b->weight, size_of(cfg->weight_type)) ||
-        !aligned(b->rstd, 4) || !aligned(b->dw, 4) || !aligned(b->workspace, 256))
+        !aligned(b->rstd, 4) || !aligned(b->workspace, 256))
       return WD_E_ALIGN;
   }
+  if (!aligned(b->dw, 4)) return WD_E_ALIGN;
   const hipStream_t stream = static_cast<hipStream_t>(cfg->stream);
   const int64_t blocks = grad_blocks(*cfg);
   if (blocks) {
     const GradArgs a = {b->dy, b->dh, b->h, b->weight, b->rstd, b->dx, b->dw ? static_cast<float*>(b->workspace) : nullptr, cfg->rows,
                         cfg->dy_stride, cfg->dh_stride, cfg->h_stride, cfg->dx_stride, cfg->width, float(1.0 / cfg->width)};
-    by_type<Grad>(cfg->type, cfg->weight_type, cfg->width, a, unsigned(blocks), stream);
-    const int status = launched();
+    const int status = by_type<Grad>(cfg->type, cfg->weight_type, cfg->width, a, unsigned(blocks), stream);
     if (status != WD_OK) return status;
   }
-  if (b->dw) {  // (of no rows: zeros)
-    norm_grad_join_kernel<<<dim3(unsigned((cfg->width + 15) / 16)), dim3(1024), 0, stream>>>(static_cast<const float*>(b->workspace), int(blocks), cfg->width, b->dw);
-    return launched();
-  }
-  return WD_OK;
+  if (!b->dw) return WD_OK;  // (of no rows: zeros)
+  return enqueue(norm_grad_join_kernel, dim3(unsigned((cfg->width + 15) / 16)), 1024, stream, static_cast<const float*>(b->workspace), int(blocks),
+                 cfg->width, b->dw);
 }
 
 }  // extern "C"

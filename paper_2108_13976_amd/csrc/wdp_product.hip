@@ -548,13 +548,12 @@ __global__ __launch_bounds__(512) void product_panel_kernel(ProductArgs p) {
   __shared__ __attribute__((aligned(16))) float scale_b[KB][PN];
   __shared__ __attribute__((aligned(16))) uint8_t staged[8][kLineBytes];
   const int t = threadIdx.x, lane = t & 63, r16 = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.y * PN;
   for (int e = t; e < KB * PN * 8; e += 512) {
-    const int block = e / (PN * 8), row = e / 8 % PN, chunk = e & 7, col = n0 + column(row), k0 = block * WDP_BLOCK + chunk * 16;
+    const int block = e / (PN * 8), row = e / 8 % PN, chunk = e & 7, col = column(row), k0 = block * WDP_BLOCK + chunk * 16;
     lds_b[block][place(row, chunk)] = col < p.n ? load_chunk(p.b + int64_t(col) * p.b_stride, k0, p.k - k0, p.aligned) : i32x4{0, 0, 0, 0};
   }
   for (int e = t; e < KB * PN; e += 512) {
-    const int block = e / PN, row = e % PN, col = n0 + column(row);
+    const int block = e / PN, row = e % PN, col = column(row);
     scale_b[block][row] = col < p.n && block < p.blocks ? p.b_scale[int64_t(p.by_row ? col : col / WDP_BLOCK) * p.bs_row + block * p.bs_block] : 0.0f;
   }
   __syncthreads();
@@ -588,7 +587,7 @@ __global__ __launch_bounds__(512) void product_panel_kernel(ProductArgs p) {
     if (tile + step < p.m_tiles) request(tile + step);
 #pragma unroll
     for (int line = 0; line < PN / kCols; ++line) {
-      const int c0 = n0 + line * kCols;
+      const int c0 = line * kCols;
       if (c0 >= p.n) break;
 #pragma unroll
       for (int pair = 0; pair < kPairs; ++pair) {
@@ -616,24 +615,24 @@ __global__ __launch_bounds__(512) void product_panel_kernel(ProductArgs p) {
   }
 }
 
-template <int FA, int FB, typename C, int BM, int BN, int WM, int WN> void launch_tiles(ProductArgs p, hipStream_t stream) {
+template <int FA, int FB, typename C, int BM, int BN, int WM, int WN> int launch_tiles(ProductArgs p, hipStream_t stream) {
   p.m_tiles = (p.m + BM - 1) / BM;
   p.n_tiles = (p.n + BN - 1) / BN;
-  product_tile_kernel<FA, FB, C, BM, BN, WM, WN><<<dim3(unsigned(p.m_tiles) * unsigned(p.n_tiles)), dim3(64 * WM * WN), 0, stream>>>(p);
+  return enqueue(product_tile_kernel<FA, FB, C, BM, BN, WM, WN>, dim3(unsigned(p.m_tiles) * unsigned(p.n_tiles)), 64 * WM * WN, stream, p);
 }
-template <int FA, int FB, bool ROWS, typename C, int BM, int BN, int WM, int WN> void launch_large(ProductArgs p, hipStream_t stream) {
+template <int FA, int FB, bool ROWS, typename C, int BM, int BN, int WM, int WN> int launch_large(ProductArgs p, hipStream_t stream) {
   p.m_tiles = (p.m + BM - 1) / BM;
   p.n_tiles = (p.n + BN - 1) / BN;
-  product_large_kernel<FA, FB, ROWS, C, BM, BN, WM, WN><<<dim3(unsigned(p.m_tiles) * unsigned(p.n_tiles)), dim3(64 * WM * WN), 0, stream>>>(p);
+  return enqueue(product_large_kernel<FA, FB, ROWS, C, BM, BN, WM, WN>, dim3(unsigned(p.m_tiles) * unsigned(p.n_tiles)), 64 * WM * WN, stream, p);
 }
-template <int FA, int FB, typename C, int TM, int TN, int WAVES, int DEPTH> void launch_stream(const ProductArgs& p, hipStream_t stream) {
-  product_stream_kernel<FA, FB, C, TM, TN, WAVES, DEPTH>
-      <<<dim3(unsigned((p.n + 16 * TN - 1) / (16 * TN)), unsigned((p.m + 16 * TM - 1) / (16 * TM))), dim3(64 * WAVES), 0, stream>>>(p);
+template <int FA, int FB, typename C, int TM, int TN, int WAVES, int DEPTH> int launch_stream(const ProductArgs& p, hipStream_t stream) {
+  return enqueue(product_stream_kernel<FA, FB, C, TM, TN, WAVES, DEPTH>,
+                 dim3(unsigned((p.n + 16 * TN - 1) / (16 * TN)), unsigned((p.m + 16 * TM - 1) / (16 * TM))), 64 * WAVES, stream, p);
 }
-template <int FA, int FB, typename C, int PN, int KB> void launch_panel(ProductArgs p, hipStream_t stream) {
+template <int FA, int FB, typename C, int PN, int KB> int launch_panel(ProductArgs p, hipStream_t stream) {
   p.m_tiles = (p.m + 31) / 32;
-  const int panels = (p.n + PN - 1) / PN, groups = (p.m_tiles + 7) / 8, most = 512 / panels;
-  product_panel_kernel<FA, FB, C, PN, KB><<<dim3(unsigned(groups < most ? groups : most > 0 ? most : 1), unsigned(panels)), dim3(512), 0, stream>>>(p);
+  const int groups = (p.m_tiles + 7) / 8;
+  return enqueue(product_panel_kernel<FA, FB, C, PN, KB>, dim3(unsigned(groups < 512 ? groups : 512)), 512, stream, p);
 }
 
 // Which kernel, by sizes and alignment (us on this card; k in blocks of 128).
@@ -649,7 +648,7 @@ template <int FA, int FB, typename C, int PN, int KB> void launch_panel(ProductA
 //     at 1.2 (1.0 with one tile a CU at most), 1024 of 64 x 64 at 1.5 (0.95, 0.65 with two, one a CU); exact ones 2.0 and
 //     1.5.  4096^3: 67 against 75 and (64) 100; 2048 x 2048 x 2000: 35, 19, 25; 1000^3: 19, 10.5, 8.3.  Columns up to 64
 //     leave half of a wider tile empty: 500000 x 64 x 300 takes 58 against 50.
-template <int FA, int FB, typename C> void launch_slice(const ProductArgs& p, hipStream_t stream) {
+template <int FA, int FB, typename C> int launch_slice(const ProductArgs& p, hipStream_t stream) {
   constexpr bool EXACT = sizeof(C) == 4;
   const auto tiles = [&](int64_t m, int64_t n) { return (p.m + m - 1) / m * ((p.n + n - 1) / n); };
   const auto rounds = [](int64_t tiles, int at_once) { return double((tiles + at_once - 1) / at_once); };
@@ -676,11 +675,11 @@ template <int FA, int FB, typename C> void launch_slice(const ProductArgs& p, hi
     if (p.by_row && p.m >= 128 && cost128 < cost64) return launch_large<FA, FB, true, C, 128, 128, 2, 2>(p, stream);
   }
   if (!p.by_row && p.m >= 128 && cost128 < cost64) return launch_large<FA, FB, false, C, 128, 128, 2, 2>(p, stream);
-  launch_large<FA, FB, true, C, 64, 64, 2, 2>(p, stream);
+  return launch_large<FA, FB, true, C, 64, 64, 2, 2>(p, stream);
 }
 
 // (a launch takes up to 2^22 tiles of 128 x 128: all sizes of a grid, and rows counted in 32 bits, stay far from their limits)
-template <int FA, int FB, typename C> void launch(const ProductArgs& p, hipStream_t stream) {
+template <int FA, int FB, typename C> int launch(const ProductArgs& p, hipStream_t stream) {
   const int64_t rows = p.m, most = (int64_t(1) << 22) / ((p.n + 127) / 128) * 128;
   for (int64_t at = 0; at < rows; at += most) {
     ProductArgs q = p;
@@ -688,13 +687,14 @@ template <int FA, int FB, typename C> void launch(const ProductArgs& p, hipStrea
     q.a_scale += at * p.as_row;
     q.c = static_cast<C*>(p.c) + at * p.c_stride;
     q.m = int32_t(rows - at < most ? rows - at : most);
-    launch_slice<FA, FB, C>(q, stream);
+    const int status = launch_slice<FA, FB, C>(q, stream);
+    if (status != WD_OK) return status;
   }
+  return WD_OK;
 }
-template <int FA, int FB> void launch_c(const ProductArgs& p, int c_type, hipStream_t stream) {
-  if (c_type == WDP_F32) launch<FA, FB, float>(p, stream);
-  else if (c_type == WDP_BF16) launch<FA, FB, bf16>(p, stream);
-  else launch<FA, FB, f16>(p, stream);
+template <int FA, int FB> int launch_c(const ProductArgs& p, int c_type, hipStream_t stream) {
+  if (c_type == WDP_F32) return launch<FA, FB, float>(p, stream);
+  return c_type == WDP_BF16 ? launch<FA, FB, bf16>(p, stream) : launch<FA, FB, f16>(p, stream);
 }
 
 int check(const wdp_product_config& c) {
@@ -734,11 +734,9 @@ int wdp_product(const wdp_product_config* cfg, const wdp_product_buffers* b) {
                          int32_t(cfg->m), cfg->n, cfg->k, (cfg->k + WDP_BLOCK - 1) / WDP_BLOCK, 0, 0,
                          aligned(b->a, 16) && aligned(b->b, 16) && cfg->a_stride % 16 == 0 && cfg->b_stride % 16 == 0, cfg->b_scale_rows == 1};
   const hipStream_t stream = static_cast<hipStream_t>(cfg->stream);
-  if (cfg->a_type == WDP_E4M3 && cfg->b_type == WDP_E4M3) launch_c<0, 0>(p, cfg->c_type, stream);
-  else if (cfg->a_type == WDP_E4M3) launch_c<0, 1>(p, cfg->c_type, stream);
-  else if (cfg->b_type == WDP_E4M3) launch_c<1, 0>(p, cfg->c_type, stream);
-  else launch_c<1, 1>(p, cfg->c_type, stream);
-  return launched();
+  const bool wide_a = cfg->a_type == WDP_E5M2, wide_b = cfg->b_type == WDP_E5M2;
+  if (wide_a) return wide_b ? launch_c<1, 1>(p, cfg->c_type, stream) : launch_c<1, 0>(p, cfg->c_type, stream);
+  return wide_b ? launch_c<0, 1>(p, cfg->c_type, stream) : launch_c<0, 0>(p, cfg->c_type, stream);
 }
 
 }  // extern "C"

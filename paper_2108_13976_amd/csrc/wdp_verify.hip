@@ -7,9 +7,10 @@
 //
 // Forms by the vocabulary.  Few actions (a policy of Tag has five): a lane a sequence, the row in its registers.  Up to
 // 1024: sixteen lanes (256) or a wave a sequence, no barrier (50000 x 2 x 100: 24 us with a wave each, 13 with sixteen
-// lanes).  Up to 4096: a workgroup.  Longer rows: a wave a piece of 1024
-// elements sums it, a second launch finds the piece that holds the drawn token and goes through that one alone.  Memory
-// bounds the large batches, the chain of dependent loads (drafts, their elements, the row, the token) the small ones.
+// lanes).  Up to 4096: a workgroup.  Longer rows: a wave a piece of 1024 elements sums it, a second launch finds the piece
+// that holds the drawn token and goes through that one alone.  Memory bounds the large batches (2000000 x 1 x 5: 24 us,
+// 5.6 TB/s), the chain of dependent loads (drafts, their elements, the row, the token) the small ones (64 x 4 x 50000:
+// 7.6 us and 4.6).
 #include "wdp_common.h"
 
 namespace wdp {
@@ -379,24 +380,27 @@ template <typename T> __global__ __launch_bounds__(64) void verify_find_kernel(V
 }
 
 // (a launch takes 2^22 sequences: all sizes of a grid stay far from their limits)
-template <typename T> void launch(VerifyArgs a, hipStream_t stream) {
+template <typename T> int launch(VerifyArgs a, hipStream_t stream) {
   const int64_t end = a.batch, most = int64_t(1) << 22;
   for (; a.start < end; a.start += most) {
     a.batch = end - a.start < most ? end : a.start + most;
     const unsigned count = unsigned(a.batch - a.start);
+    int status;
     const auto blocks = [&](unsigned each) { return dim3((count + each - 1) / each); };
-    if (a.vocab <= 8 && a.drafts == 1 && !a.bonus) verify_lane_kernel<T, 8, true><<<blocks(256), 256, 0, stream>>>(a);
-    else if (a.vocab <= 8) verify_lane_kernel<T, 8, false><<<blocks(256), 256, 0, stream>>>(a);
-    else if (a.vocab <= 64) verify_group_kernel<T, 16, 4><<<blocks(16), 256, 0, stream>>>(a);
-    else if (a.vocab <= 128) verify_group_kernel<T, 16, 8><<<blocks(16), 256, 0, stream>>>(a);
-    else if (a.vocab <= 256) verify_group_kernel<T, 16, 16><<<blocks(16), 256, 0, stream>>>(a);
-    else if (a.vocab <= 1024) verify_group_kernel<T, 64, 16><<<blocks(4), 256, 0, stream>>>(a);
-    else if (a.vocab <= kRow) verify_row_kernel<T, 4><<<dim3(count), 256, 0, stream>>>(a);
+    if (a.vocab <= 8 && a.drafts == 1 && !a.bonus) status = enqueue(verify_lane_kernel<T, 8, true>, blocks(256), 256, stream, a);
+    else if (a.vocab <= 8) status = enqueue(verify_lane_kernel<T, 8, false>, blocks(256), 256, stream, a);
+    else if (a.vocab <= 64) status = enqueue(verify_group_kernel<T, 16, 4>, blocks(16), 256, stream, a);
+    else if (a.vocab <= 128) status = enqueue(verify_group_kernel<T, 16, 8>, blocks(16), 256, stream, a);
+    else if (a.vocab <= 256) status = enqueue(verify_group_kernel<T, 16, 16>, blocks(16), 256, stream, a);
+    else if (a.vocab <= 1024) status = enqueue(verify_group_kernel<T, 64, 16>, blocks(4), 256, stream, a);
+    else if (a.vocab <= kRow) status = enqueue(verify_row_kernel<T, 4>, dim3(count), 256, stream, a);
     else {
-      verify_sums_kernel<T><<<dim3(unsigned((a.pieces + 3) / 4), count < 32768 ? count : 32768, (count + 32767) / 32768), 256, 0, stream>>>(a, end);
-      verify_find_kernel<T><<<dim3(count), 64, 0, stream>>>(a, end);
+      status = enqueue(verify_sums_kernel<T>, dim3(unsigned((a.pieces + 3) / 4), count < 32768 ? count : 32768, (count + 32767) / 32768), 256, stream, a, end);
+      if (status == WD_OK) status = enqueue(verify_find_kernel<T>, dim3(count), 64, stream, a, end);
     }
+    if (status != WD_OK) return status;
   }
+  return WD_OK;
 }
 
 int pieces_of(const wdp_verify_config& c) { return c.vocab <= kRow ? 0 : (c.vocab + kPiece - 1) / kPiece; }
@@ -443,10 +447,8 @@ int wdp_verify(const wdp_verify_config* cfg, const wdp_verify_buffers* b) {
                         0, cfg->batch, cfg->target_batch_stride, cfg->target_row_stride, cfg->draft_batch_stride, cfg->draft_row_stride,
                         cfg->drafts, cfg->vocab, cfg->bonus, pieces};
   const hipStream_t stream = static_cast<hipStream_t>(cfg->stream);
-  if (cfg->type == WDP_F32) launch<float>(a, stream);
-  else if (cfg->type == WDP_BF16) launch<bf16>(a, stream);
-  else launch<f16>(a, stream);
-  return launched();
+  if (cfg->type == WDP_F32) return launch<float>(a, stream);
+  return cfg->type == WDP_BF16 ? launch<bf16>(a, stream) : launch<f16>(a, stream);
 }
 
 }  // extern "C"

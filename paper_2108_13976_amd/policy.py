@@ -2,7 +2,8 @@
 
 First the C ABI, one Python function per entry point; then functions on torch tensors, which check their arguments,
 allocate outputs and workspaces and run on the tensors' device, on its current stream.  Every step runs in libwd's HIP
-kernels; without a GPU the tensor functions raise.
+kernels; without a GPU the tensor functions raise.  They record nothing for autograd: the way back is rms_norm_backward
+and product8 with the operands that the gradients need.
 """
 import collections
 import ctypes
@@ -500,6 +501,17 @@ class AdamW:
         for p, g in zip(params, grads):
             if g.dtype not in (torch.float32, p.dtype):
                 raise ValueError(f"{what}: a gradient has type {g.dtype}, its parameter {p.dtype}")
+
+        # what is written lies apart from everything else: a tensor that stands twice would be updated by two workgroups at once
+        spans = []
+        for written, tensors in ((True, params), (False, grads), (True, self.masters), (True, self.exp_avg), (True, self.exp_avg_sq),
+                                 (True, self.avg_scale), (True, self.sq_scale)):
+            spans += [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), written) for t in tensors or () if t.numel()]
+        end, end_written = 0, 0  # of everything before, and of what is written of it
+        for start, stop, written in sorted(spans):
+            if start < (end if written else end_written):
+                raise ValueError(f"{what}: tensors overlap (a shared parameter stands once, its gradients summed)")
+            end, end_written = max(end, stop), max(end_written, stop if written else 0)
 
         def ptr(tensors, i):
             return tensors[i].data_ptr() if tensors is not None else None

@@ -807,3 +807,54 @@ def test_norm_and_its_gradients_in_place_where_the_row_ends_inside_a_chunk(width
         wd.wdp_norm_backward(cfg, policy.wdp_norm_grad_buffers(first.data_ptr(), second.data_ptr(), h.data_ptr(), w.data_ptr(), rstd.data_ptr(), to.data_ptr(),
                                                                dw2.data_ptr(), space.data_ptr()))
         assert torch.equal(to, dx) and torch.equal(dw2, dw), over_dy
+
+
+def test_an_earlier_error_of_the_program_is_not_the_operators():
+    """A runtime call that failed leaves its status behind (here: a device that does not exist); the operators answer for their own launches."""
+    hip = ctypes.CDLL("libamdhip64.so")
+    calls, _ = one_of_each(generator(33))
+    params, grads = tensors_of(generator(34), [100], F32)
+    optimiser = wd.AdamW(params, grads)
+    want = [t.clone() for t in calls()]
+    torch.cuda.synchronize()
+    assert hip.hipSetDevice(4096) != 0
+    c = policy.wdp_adamw_config(ctypes.sizeof(policy.wdp_adamw_config), 32, 1e-3, 0.9, 0.999, 1e-8, 0.01, 1, None, None, 0, None)
+    wd.wdp_adamw(c, optimiser._table, 1)
+    got = calls()
+    assert hip.hipGetLastError() != 0  # (still there; torch's own launches would answer with it)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_adamw_refuses_tensors_that_overlap():
+    params, grads = tensors_of(generator(35), [300, 300], F32)
+    flat = torch.zeros(500, device=DEV)
+    for call in (lambda: wd.AdamW([params[0], params[0]], grads), lambda: wd.AdamW([flat[:300], flat[200:]], grads), lambda: wd.AdamW(params, [grads[0], params[0]]),
+                 lambda: wd.AdamW(params, grads, exp_avg=[flat[:300], flat[200:]], exp_avg_sq=[torch.zeros(300, device=DEV) for _ in range(2)]),
+                 lambda: wd.AdamW(params[:1], grads[:1], masters=params[:1])):
+        with pytest.raises(ValueError):
+            call()
+    wd.AdamW(params, [grads[0], grads[0]]).step()  # (a gradient is read only)
+    wd.AdamW([flat[:300], flat[300:]], [grads[0], grads[1][:200]]).step()
+
+
+def test_adamw_of_one_tensor_beyond_a_launch():
+    """2^34 elements and a few: more than one launch's workgroups."""
+    many = (1 << 34) + 5000
+    if torch.cuda.mem_get_info()[0] < 7 * many:
+        pytest.skip("needs 120 GB of free memory")
+    param, grad = torch.ones(many, dtype=BF16, device=DEV), torch.full((many,), 0.5, dtype=BF16, device=DEV)
+    opt = wd.AdamW([param], [grad], lr=0.25, weight_decay=0.0, state_bits=8)
+    opt.step()
+    # m = 0.05, s = sqrt(0.001) / 2, the update lr * 1, p = 0.75; scale max / 448, and codes 448, or 416 below it where a quotient
+    # that its roundings left just under 448 meets sixteen random zeros
+    for at in (0, (1 << 33) - 4096, (1 << 34) - 4096, (1 << 34) - 100, many - 4096):
+        part = slice(at, at + 4096)
+        assert (param[part] == 0.75).all(), at
+        for codes in (opt.exp_avg[0][part].float(), opt.exp_avg_sq[0][part].float()):
+            assert ((codes == 448) | (codes == 416)).all() and int((codes == 416).sum()) < 8, at
+    for scales, value in ((opt.avg_scale[0], 0.05), (opt.sq_scale[0], 0.5 * 0.001 ** 0.5)):
+        low, high = torch.aminmax(scales)
+        assert low == high and abs(float(low) * 448 / value - 1) < 1e-5
+    del param, grad, opt, part, codes, scales, low, high
+    torch.cuda.empty_cache()

@@ -315,3 +315,13 @@ def test_kernels_keep_their_state_in_registers(notes):  # noqa: F811
     for part in ("norm_kernel", "norm_grad_kernel", "norm_grad_join_kernel", "product_tile_kernel", "product_large_kernel", "product_stream_kernel",
                  "product_panel_kernel", "verify_lane_kernel", "verify_group_kernel", "verify_row_kernel", "verify_sums_kernel", "verify_find_kernel", "adamw_kernel"):
         assert any(part in m for m in found), part
+
+
+def test_scales_of_a_norm_lie_apart():
+    assert status(wd.wdp_norm, norm_config(scale_row_stride=0), norm_buffers()) == CONFIG
+    wide = dict(width=200, x_stride=200, residual_stride=200, h_stride=200, y_stride=200, q_stride=208)
+    assert status(wd.wdp_norm, norm_config(scale_block_stride=0, **wide), norm_buffers()) == CONFIG
+
+
+def test_gradients_of_no_rows_are_checked_too():
+    assert status(wd.wdp_norm_backward, norm_config(rows=0), grad_buffers(dw=P + 4098)) == ALIGN
