@@ -291,10 +291,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile_kernel(ProductAr
 // 1 KB, eight rows; the lane that fills a place asks for the chunk that belongs there), a block ahead.
 //
 // 256 x 256 with eight waves of 128 x 64: a block is 2048 cycles of a SIMD's matrix core beside 1024 of its vector
-// unit; LDS is in use for a seventh of the time (no bank conflicts).  The results of an instruction are added three
+// unit; LDS for all of it (192 KB read, 64 KB written; no bank conflicts).  The results of an instruction are added three
 // instructions later, or the wave stands still for the matrix core's latency (8192 x 8192 x 4096: 304 us against 283).
-// Without its loads that product takes 249 us, of which 27 are c's 128 MB at a copy's rate: the matrix core, slowed by
-// its clock, is what is left.  Two blocks ahead or three (with fewer workgroups a CU) are slower for every size.
+// Two blocks ahead or three (with fewer workgroups a CU) are slower for every size.
 //
 // Scales: without ROWS (a wave's columns share one) they are requested into registers a block ahead; with ROWS, one for
 // each column, both kinds come by way of LDS (5000 x 333 x 1000 with float32 results: 13.2 us by registers, 11.6).
@@ -433,6 +432,168 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_large_kernel(ProductA
   }
   __syncthreads();
   store_tile<C>(p, reinterpret_cast<uint8_t*>(lds) + wave * kLineBytes, lane, m0 + wm, n0 + wn, acc);
+}
+
+// ---- large tiles, long k -----------------------------------------------------------------------------------
+// The tiles above spend a third of a long product's time at the changes of blocks: all waves ask LDS for their first
+// fragments at once (12 KB each, 768 cycles of LDS) and the matrix core waits.  Here the change lies inside a block's
+// multiplications: once a wave has read the last of a block's rows (three rows of instructions before its end) it waits for
+// the next block's chunks, and reads of those what it has registers for as their last uses pass: the columns one by one, then
+// the first rows.  The last rows are therefore multiplied column by column, those before row by row.
+//
+// 3000^3, a scale a column (128 x 128): 66 us, here 57; 8192 x 8192 x 4096 (256 x 256): 270, 258; 3000 x 3000 x 768: 19.3,
+// 17.9; but x 256: 10.2, 10.8, and with float32 results, whose fragments are twice as large, 2000 x 2000 x 4096: 44, 49.
+// What is left at 8192 x 8192 x 4096: without its requests 208 us, with every second of them 237, with all of them to lines
+// that L2 holds 247: their way to LDS, which is busy for all of the matrix core's 2048 cycles a block (192 KB read, 64 KB
+// written); without the results' stores 242.  On operands of zeros, where the clock stays up, the same instructions are a third
+// faster.
+//
+// f(0), f(1), ... with constants.
+template <int FROM, int TO, typename F> __device__ __forceinline__ void steps(const F& f) {
+  if constexpr (FROM < TO) {
+    f(std::integral_constant<int, FROM>{});
+    steps<FROM + 1, TO>(f);
+  }
+}
+
+// v, where it is used: addresses made from it are not kept in registers from block to block (a 32-bit offset beside a
+// scalar base is one register where the lane's address would be two for each of eight requests).
+__device__ __forceinline__ uint32_t here(uint32_t v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+template <int FA, int FB, bool ROWS, typename C, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_long_kernel(ProductArgs p) {
+  static_assert(sizeof(C) == 2, "8-bit instructions");
+  constexpr int kWaves = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+  constexpr int kA = BM / 8 / kWaves, kB = BN / 8 / kWaves;  // eights of rows that a wave brings
+  static_assert(BM % 64 == 0 && BN % 64 == 0 && BM / 64 + BN / 64 <= kWaves && kA % 2 == 0 && kB % 2 == 0, "a wave brings 64 scales at most");
+  // (four objects, not one in halves: the compiler then knows that reading one does not wait for requests into the other)
+  __shared__ i32x4 even[(BM + BN) * 8], odd[(BM + BN) * 8];
+  __shared__ __attribute__((aligned(16))) float even_scales[BM + BN], odd_scales[BM + BN];
+  static_assert(sizeof(even) >= kWaves / 2 * kLineBytes, "results are staged there");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int mt, nt;
+  tile_of(p, &mt, &nt);
+  // the last tile of rows ends with the last row: it computes some rows that its neighbour computes too, alike
+  const int m0 = mt * BM + BM <= p.m ? mt * BM : p.m - BM, n0 = nt * BN;
+  const int wm = (wave % WM) * TM * 16, wn = (wave / WM) * TN * 16;
+  const int r16 = lane & 15, g = lane >> 4;
+  // Of a wave's eights of rows a lane asks for the chunk of row lane / 8 that belongs at place lane % 8; in odd eights it is the
+  // chunk four further or back.  (column() moves bits: it is the sum of what the eight and the lane make of it.)
+  const uint32_t from_a = uint32_t(lane >> 3) * uint32_t(p.a_stride), from_b = uint32_t(column(lane >> 3)) * uint32_t(p.b_stride);
+  const uint8_t* tile_a = p.a + int64_t(m0 + wave * kA * 8) * p.a_stride;
+  const uint8_t* tile_b = p.b + int64_t(n0) * p.b_stride;
+  // the first waves bring the scales of a, the next those of b
+  const int first = n0 + (wave - BM / 64) * 64, base = first < p.n ? first : p.n - 1;
+  const float* tile_scale = wave < BM / 64 ? p.a_scale + int64_t(m0 + wave * 64) * p.as_row : p.b_scale + int64_t(p.by_row ? base : base / WDP_BLOCK) * p.bs_row;
+  const int64_t scale_block = wave < BM / 64 ? p.as_block : p.bs_block;
+  const int col = first + column(lane) < p.n ? first + column(lane) : p.n - 1;
+  const uint32_t from_scale = wave < BM / 64 ? uint32_t(lane) * uint32_t(p.as_row) : p.by_row ? uint32_t(col - base) * uint32_t(p.bs_row) : 0u;
+  auto request = [&](int block, i32x4* lds, float* scales) {
+    const int k0 = block * WDP_BLOCK;
+    if (wave < BM / 64 + BN / 64) to_lds(tile_scale + block * scale_block + here(from_scale), scales + wave * 64);
+    const uint8_t *a = tile_a + k0, *b = tile_b + k0;
+    i32x4 *to_a = lds + wave * kA * 64, *to_b = lds + BM * 8 + wave * kB * 64;
+    const int l = int(here(uint32_t(lane))), chunks[2] = {((l & 7) ^ (l >> 4)) * 16, ((l & 7) ^ (l >> 4) ^ 4) * 16};
+    if ((k0 + WDP_BLOCK <= p.k) & (n0 + BN <= p.n)) {
+#pragma unroll
+      for (int i = 0; i < kA; ++i) to_lds(a + i * 8 * p.a_stride + (here(from_a) + chunks[i & 1]), to_a + i * 64);
+#pragma unroll
+      for (int i = 0; i < kB; ++i) to_lds(b + column((wave * kB + i) * 8) * p.b_stride + (here(from_b) + chunks[i & 1]), to_b + i * 64);
+    } else {
+      // at the end of k zeros in place of chunks with nothing of the row, at the end of n the last column
+      const uint8_t* zeros = reinterpret_cast<const uint8_t*>(&kZeros);
+#pragma unroll
+      for (int i = 0; i < kA; ++i) to_lds(k0 + chunks[i & 1] < p.k ? a + i * 8 * p.a_stride + (here(from_a) + chunks[i & 1]) : zeros, to_a + i * 64);
+#pragma unroll
+      for (int i = 0; i < kB; ++i) {
+        const int col = column((wave * kB + i) * 8) + column(l >> 3);
+        const uint32_t row = uint32_t(n0 + col < p.n ? col : p.n - 1 - n0) * uint32_t(p.b_stride);
+        to_lds(k0 + chunks[i & 1] < p.k ? b + (row + chunks[i & 1]) : zeros, to_b + i * 64);
+      }
+    }
+  };
+  auto arrived = [&](int block, i32x4* lds) {  // everyone's requests for the block, and everyone is through with the other one
+    __syncthreads();
+    if ((block + 1 == p.blocks) & ((p.k & 15) != 0)) {
+      // zeros in place of the bytes behind the row in its last chunk
+      for (int row = threadIdx.x; row < BM + BN; row += 64 * kWaves) {
+        i32x4* at = lds + place(row, (p.k & (WDP_BLOCK - 1)) >> 4);
+        *at = first_bytes(*at, p.k & 15);
+      }
+      __syncthreads();
+    }
+  };
+  // a lane's chunks of the wave's first sixteen rows and columns (sixteen rows further they lie 128 chunks further)
+  const uint32_t first_a = uint32_t(place(wm + r16, g)), first_b = uint32_t(place(BM + wn + r16, g));
+  auto load_a = [&](const i32x4* lds, uint32_t at, int i) { return fragment<FA, false>(lds[at + 128 * i], lds[(at ^ 4) + 128 * i]); };
+  auto load_b = [&](const i32x4* lds, uint32_t at, int j) { return fragment<FB, false>(lds[at + 128 * j], lds[(at ^ 4) + 128 * j]); };
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  constexpr int kDelay = 3, kSlots = TM == 8 ? 3 : TM / 2, kTop = (TM - kSlots) * TN;
+  Fragment<false> fa[kSlots], fb[TN];
+  request(0, even, even_scales);
+  arrived(0, even);
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) fa[i] = load_a(even, first_a, i);
+#pragma unroll
+  for (int j = 0; j < TN; ++j) fb[j] = load_b(even, first_b, j);
+  if (p.blocks > 1) request(1, odd, odd_scales);
+  const auto multiply = [&](int block, i32x4* lds, float* scales, i32x4* other) {
+    const uint32_t own_a = here(first_a), row = here(uint32_t(wm + r16));
+    uint32_t next_a, next_b;
+    float sa[TM];
+    f32x4 sb[ROWS ? TN : 1];
+    const float shared = ROWS ? 1.0f : scales[BM + wn];  // the wave's columns have one scale
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = ROWS ? scales[row + i * 16] : scales[row + i * 16] * shared;
+    if (ROWS) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sb[j] = *reinterpret_cast<const f32x4*>(&scales[BM + wn + j * 16 + g * 4]);
+    }
+    f32x4 part[kDelay + 1];
+    const auto step = [&](auto at) {
+      constexpr int e = decltype(at)::value;
+      constexpr auto row_of = [](int e) { return e < kTop ? e / TN : TM - kSlots + ((e - kTop) % kSlots + kSlots - TM % kSlots) % kSlots; };
+      constexpr auto col_of = [](int e) { return e < kTop ? e % TN : (e - kTop) / kSlots; };
+      if constexpr (e < TM * TN) {
+        constexpr int i = row_of(e), j = col_of(e);
+        part[e % (kDelay + 1)] = inner<FA, FB, false>(fb[j], fa[i % kSlots]);
+        if (e < kTop && j == TN - 1) fa[i % kSlots] = load_a(lds, own_a, i + kSlots);
+        if (e >= kTop && (e - kTop) % kSlots == kSlots - 1 && j > 0) fb[j] = load_b(other, next_b, j);
+        if (e >= kTop && j == TN - 1) fa[i % kSlots] = load_a(other, next_a, i % kSlots);
+      }
+      if constexpr (e >= kDelay) {
+        constexpr int d = e - kDelay, i = row_of(d), j = col_of(d);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) acc[i][j][x] = fmaf(part[d % (kDelay + 1)][x], ROWS ? sa[i] * sb[ROWS ? j : 0][x] : sa[i], acc[i][j][x]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr int kChange = kTop + kSlots;
+    steps<0, kChange>(step);
+    // (the sums so far are made here: the compiler would sink them behind the branches and keep all the products instead)
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(acc[i][j]));
+    arrived(block + 1, other);
+    if (block + 2 < p.blocks) request(block + 2, lds, scales);
+    next_a = here(first_a), next_b = here(first_b);
+    fb[0] = load_b(other, next_b, 0);
+    steps<kChange, TM * TN + kDelay>(step);
+  };
+  for (int block = 0; block < p.blocks; block += 2) {
+    multiply(block, even, even_scales, odd);
+    if (block + 1 < p.blocks) multiply(block + 1, odd, odd_scales, even);
+  }
+  __syncthreads();
+  store_tile<C>(p, reinterpret_cast<uint8_t*>(wave < kWaves / 2 ? even : odd) + wave % (kWaves / 2) * kLineBytes, lane, m0 + wm, n0 + wn, acc);
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------
@@ -625,6 +786,11 @@ template <int FA, int FB, bool ROWS, typename C, int BM, int BN, int WM, int WN>
   p.n_tiles = (p.n + BN - 1) / BN;
   return enqueue(product_large_kernel<FA, FB, ROWS, C, BM, BN, WM, WN>, dim3(unsigned(p.m_tiles) * unsigned(p.n_tiles)), 64 * WM * WN, stream, p);
 }
+template <int FA, int FB, bool ROWS, typename C, int BM, int BN, int WM, int WN> int launch_long(ProductArgs p, hipStream_t stream) {
+  p.m_tiles = (p.m + BM - 1) / BM;
+  p.n_tiles = (p.n + BN - 1) / BN;
+  return enqueue(product_long_kernel<FA, FB, ROWS, C, BM, BN, WM, WN>, dim3(unsigned(p.m_tiles) * unsigned(p.n_tiles)), 64 * WM * WN, stream, p);
+}
 template <int FA, int FB, typename C, int TM, int TN, int WAVES, int DEPTH> int launch_stream(const ProductArgs& p, hipStream_t stream) {
   return enqueue(product_stream_kernel<FA, FB, C, TM, TN, WAVES, DEPTH>,
                  dim3(unsigned((p.n + 16 * TN - 1) / (16 * TN)), unsigned((p.m + 16 * TM - 1) / (16 * TM))), 64 * WAVES, stream, p);
@@ -671,8 +837,15 @@ template <int FA, int FB, typename C> int launch_slice(const ProductArgs& p, hip
   const double cost128 = t128 <= 256 ? 1.0 : (EXACT ? 2.0 : 1.17) * rounds(t128, 512), cost256 = 2.1 * rounds(t256, 256);
   if (p.n <= 64) cost64 = 0.0;
   if constexpr (!EXACT) {
-    if (!p.by_row && p.m >= 256 && cost256 < cost128 && cost256 < cost64) return launch_large<FA, FB, false, C, 256, 256, 2, 4>(p, stream);
-    if (p.by_row && p.m >= 128 && cost128 < cost64) return launch_large<FA, FB, true, C, 128, 128, 2, 2>(p, stream);
+    const bool longer = p.blocks >= 6 && p.as_row <= (1 << 23) && p.bs_row <= (1 << 23);
+    if (!p.by_row && p.m >= 256 && cost256 < cost128 && cost256 < cost64) {
+      if (longer) return launch_long<FA, FB, false, C, 256, 256, 2, 4>(p, stream);
+      return launch_large<FA, FB, false, C, 256, 256, 2, 4>(p, stream);
+    }
+    if (p.by_row && p.m >= 128 && cost128 < cost64) {
+      if (longer) return launch_long<FA, FB, true, C, 128, 128, 2, 2>(p, stream);
+      return launch_large<FA, FB, true, C, 128, 128, 2, 2>(p, stream);
+    }
   }
   if (!p.by_row && p.m >= 128 && cost128 < cost64) return launch_large<FA, FB, false, C, 128, 128, 2, 2>(p, stream);
   return launch_large<FA, FB, true, C, 64, 64, 2, 2>(p, stream);

@@ -858,3 +858,30 @@ def test_adamw_of_one_tensor_beyond_a_launch():
         assert low == high and abs(float(low) * 448 / value - 1) < 1e-5
     del param, grad, opt, part, codes, scales, low, high
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("m,n,k,by_row,a_type,b_type,dtype", [
+    (3000, 2999, 777, False, E4M3, E4M3, BF16), (2817, 3000, 768, False, E5M2, E4M3, F16), (2900, 2881, 1028, False, E4M3, E5M2, BF16), (3000, 3001, 900, False, E5M2, E5M2, BF16),
+    (3000, 2999, 777, True, E4M3, E4M3, BF16), (1500, 1537, 768, True, E5M2, E4M3, F16), (1601, 1500, 1028, True, E4M3, E5M2, BF16), (1500, 1600, 641, True, E5M2, E5M2, BF16)])
+def test_product_of_many_blocks_of_k(m, n, k, by_row, a_type, b_type, dtype):
+    """Odd and even counts of blocks, ends inside a chunk and at one, NaN codes behind the rows, a guard around c."""
+    gen = generator(m, n, k)
+    a, a_scale, b, b_scale = operands(gen, m, n, k, a_type, b_type, by_row)
+    if dtype == F16:
+        a_scale = a_scale * 0.01
+
+    def wide(t):
+        store = torch.full((t.shape[0] + 1, -(-k // 16) * 16 + 32), 0x7F, dtype=torch.uint8, device=DEV)
+        store[:-1, :k] = t.contiguous().view(torch.uint8)
+        return store.view(t.dtype)[:-1, :k]
+
+    c = torch.full((m + 1, n + 9), 3.0, device=DEV, dtype=dtype)
+    wd.product8(wide(a), a_scale, wide(b), b_scale, out=c[:m, :n])
+    check_product(a, a_scale, b, b_scale, by_row, c[:m, :n])
+    assert (c[m:] == 3).all() and (c[:, n:] == 3).all()
+    if by_row and n < 1900:  # scales so far apart (50 GB) that their places need more than 32 bits
+        far = torch.empty_strided(b_scale.shape, ((1 << 23) + 1, 1), device=DEV)
+        far.copy_(b_scale)
+        check_product(a, a_scale, b, far, by_row, wd.product8(wide(a), a_scale, wide(b), far, dtype=dtype))
+        del far
+        torch.cuda.empty_cache()
