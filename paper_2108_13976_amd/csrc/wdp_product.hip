@@ -27,6 +27,7 @@ struct ProductArgs {
   int32_t m, n, k, blocks;  // blocks of 128 along k
   int32_t m_tiles, n_tiles;
   int32_t aligned;          // rows of a and b start at 16-byte boundaries
+  int32_t staged;           // and lie near enough for 32-bit offsets
   int32_t by_row;           // b_scale has a row for each row of b, not for 128
 };
 
@@ -597,12 +598,21 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_long_kernel(ProductAr
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------
-// b is streamed once, straight into registers: a workgroup owns 16 TN columns and 16 TM rows, its waves take the blocks of
-// k in turn, DEPTH of them requested at a time, and join their sums in LDS.
+// A workgroup owns 16 TM rows and 16 TN columns, its waves take the blocks of k in turn, DEPTH of them requested at a time,
+// and join their sums in LDS.  No barrier before that: a wave waits for its own requests alone, the other seven's are under
+// way meanwhile.
+//
+// A block's rows go through LDS though each is read once: an instruction's operand has sixteen rows in sixteen neighbouring
+// lanes, and requests in that order, sixteen bytes of sixteen lines, reach 38 GB/s a CU; eight lanes to a line reach 90 to
+// 110 (both from L2).  Straight to registers 112 x 2448 x 5632 took 18.7 us (here 11.5), 256 x 256 x 8192 9.7 (5.7),
+// 16 x 4096 x 4096 6.3 (4.8), with four blocks under way as with one.
 template <int FA, int FB, typename C, int TM, int TN, int WAVES, int DEPTH>
 __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs p) {
   constexpr bool EXACT = sizeof(C) == 4;
-  __shared__ f32x4 sums[WAVES][TM][TN][64];
+  constexpr int kRows = 16 * (TM + TN);    // of a staged block: those of a, then of b
+  constexpr bool kNear = TM * TN >= 16;    // (the largest piece is taken for near rows and scales alone: 32-bit places)
+  __shared__ i32x4 lds[WAVES * DEPTH * kRows * 8];
+  static_assert(sizeof(lds) >= WAVES * TM * TN * sizeof(f32x4) * 64, "sums are joined there");
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r16 = lane & 15, g = lane >> 4;
   const int n0 = blockIdx.x * 16 * TN, m0 = blockIdx.y * 16 * TM;
   f32x4 acc[TM][TN];
@@ -611,75 +621,116 @@ __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs 
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   // rows and columns beyond the last read the last one: their results are not stored
-  const uint8_t *a[TM], *b[TN];
-  const float *as[TM], *bs[TN][4];
+  using Place = std::conditional_t<kNear, uint32_t, int64_t>;
+  const auto scale_at = [](const float* from, Place bytes) { return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(from) + bytes); };
+  const Place a_pitch = Place(p.as_row) * 4, b_pitch = Place(p.bs_row) * 4;
+  Place as[TM], bs[TN];  // where the scales of the lane's rows of a lie; that of its first column of four
+  int more[TN];          // columns behind that
+  const float *tile_as = p.a_scale + int64_t(m0) * p.as_row, *tile_bs = p.b_scale + int64_t(p.by_row ? n0 : n0 / WDP_BLOCK) * p.bs_row;
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int row = m0 + i * 16 + r16 < p.m ? m0 + i * 16 + r16 : p.m - 1;
-    a[i] = p.a + int64_t(row) * p.a_stride + g * 16;
-    as[i] = p.a_scale + int64_t(row) * p.as_row;
-  }
+  for (int i = 0; i < TM; ++i) as[i] = Place(m0 + i * 16 + r16 < p.m ? i * 16 + r16 : p.m - 1 - m0) * a_pitch;
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
-    const int col = n0 + j * 16 + r16 < p.n ? n0 + j * 16 + r16 : p.n - 1;
-    b[j] = p.b + int64_t(col) * p.b_stride + g * 16;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {  // of the lane's results
-      const int at = n0 + j * 16 + g * 4 + e < p.n ? n0 + j * 16 + g * 4 + e : p.n - 1;
-      bs[j][e] = p.b_scale + int64_t(p.by_row ? at : at / WDP_BLOCK) * p.bs_row;
-    }
+    const int at = n0 + j * 16 + g * 4 < p.n ? n0 + j * 16 + g * 4 : p.n - 1;
+    bs[j] = Place(p.by_row ? at - n0 : at / WDP_BLOCK - n0 / WDP_BLOCK) * b_pitch;
+    more[j] = p.n - 1 - at;
   }
-  i32x4 la[DEPTH][TM][2], lb[DEPTH][TN][2];
   float sa[DEPTH][TM], sb[DEPTH][TN][4];
   auto scales = [&](int d, int block) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sa[d][i] = as[i][block * p.as_block];
+    for (int i = 0; i < TM; ++i) sa[d][i] = scale_at(tile_as + block * p.as_block, as[i]);
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      sb[d][j][0] = bs[j][0][block * p.bs_block];
+      sb[d][j][0] = scale_at(tile_bs + block * p.bs_block, bs[j]);
 #pragma unroll
-      for (int e = 1; e < 4; ++e) sb[d][j][e] = p.by_row ? bs[j][e][block * p.bs_block] : sb[d][j][0];
+      for (int e = 1; e < 4; ++e) sb[d][j][e] = p.by_row ? scale_at(tile_bs + block * p.bs_block, bs[j] + Place(e < more[j] ? e : more[j]) * b_pitch) : sb[d][j][0];
     }
   };
-  auto add = [&](int d) {
+  auto add = [&](int d, auto row_of_a, auto row_of_b) {
     Fragment<EXACT> fb[TN];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) fb[j] = fragment<FB, EXACT>(lb[d][j][0], lb[d][j][1]);
+    for (int j = 0; j < TN; ++j) fb[j] = row_of_b(j);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const Fragment<EXACT> fa = fragment<FA, EXACT>(la[d][i][0], la[d][i][1]);
+      const Fragment<EXACT> fa = row_of_a(i);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         const f32x4 part = inner<FA, FB, EXACT>(fb[j], fa);
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[e], sa[d][i] * sb[d][j][e], acc[i][j][e]);
       }
+      if (kNear) __builtin_amdgcn_sched_barrier(0);  // (a row of operands at a time in the registers)
     }
   };
-  const int whole = p.k / WDP_BLOCK;  // blocks of 128; what is left of k is one more, and a wave's of its own
-  int block = wave;
-  for (; block + (DEPTH - 1) * WAVES < whole; block += DEPTH * WAVES) {
+  if (kNear || p.staged) {  // by way of the wave's own part of LDS
+    // eights of rows, a lane the chunk of row lane / 8 that belongs at place lane % 8 (odd eights: four further or back)
+    const auto chunk_of = [](int lane) { return ((lane & 7) ^ (lane >> 4)) * 16; };
+    uint32_t from[2 * (TM + TN)];
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      const int64_t k0 = int64_t(block + d * WAVES) * WDP_BLOCK;
-#pragma unroll
-      for (int j = 0; j < TN; ++j) lb[d][j][0] = load_raw<i32x4>(b[j] + k0), lb[d][j][1] = load_raw<i32x4>(b[j] + k0 + 64);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) la[d][i][0] = load_raw<i32x4>(a[i] + k0), la[d][i][1] = load_raw<i32x4>(a[i] + k0 + 64);
-      scales(d, block + d * WAVES);
+    for (int i = 0; i < 2 * (TM + TN); ++i) {
+      const int r = (i < 2 * TM ? i : i - 2 * TM) * 8 + (lane >> 3), most = i < 2 * TM ? p.m - 1 - m0 : p.n - 1 - n0;
+      from[i] = uint32_t(r < most ? r : most) * uint32_t(i < 2 * TM ? p.a_stride : p.b_stride) + (chunk_of(lane) ^ (64 * (i & 1)));
     }
+    const uint8_t *tile_a = p.a + int64_t(m0) * p.a_stride, *tile_b = p.b + int64_t(n0) * p.b_stride;
+    i32x4* mine = lds + wave * (DEPTH * kRows * 8);
+    // (place() of sixteen rows further is 128 chunks further)
+    const uint32_t first_a = uint32_t(place(r16, g)), first_b = first_a + 128 * TM;
+    const auto of_a = [&](const i32x4* block) {
+      return [block, at = here(first_a)](int i) { return fragment<FA, EXACT>(block[at + 128 * i], block[(at ^ 4) + 128 * i]); };
+    };
+    const auto of_b = [&](const i32x4* block) {
+      return [block, at = here(first_b)](int j) { return fragment<FB, EXACT>(block[at + 128 * j], block[(at ^ 4) + 128 * j]); };
+    };
+    const int whole = p.k / WDP_BLOCK;
+    for (int block = wave; block < whole; block += DEPTH * WAVES) {
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) add(d);
+      for (int d = 0; d < DEPTH; ++d) {
+        const int at = block + d * WAVES;
+        if (d > 0 && at >= whole) break;
+#pragma unroll
+        for (int i = 0; i < 2 * (TM + TN); ++i) to_lds((i < 2 * TM ? tile_a : tile_b) + at * WDP_BLOCK + here(from[i]), mine + (d * kRows + i * 8) * 8);
+        scales(d, at);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the wave's own requests: no other wave reads them)
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        if (d > 0 && block + d * WAVES >= whole) break;
+        add(d, of_a(mine + d * kRows * 8), of_b(mine + d * kRows * 8));
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (read before the next requests may write there)
+    }
+    if (whole < p.blocks && wave == whole % WAVES) {  // what is left of k
+      const int k0 = whole * WDP_BLOCK, chunk = chunk_of(int(here(uint32_t(lane)))), end = (p.k & (WDP_BLOCK - 1)) >> 4;
+#pragma unroll
+      for (int i = 0; i < 2 * (TM + TN); ++i)  // zeros in place of chunks with nothing of the row,
+        to_lds(k0 + (chunk ^ (64 * (i & 1))) < p.k ? (i < 2 * TM ? tile_a : tile_b) + k0 + here(from[i]) : reinterpret_cast<const uint8_t*>(&kZeros), mine + i * 64);
+      scales(0, whole);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (p.k & 15) {  // and of the bytes behind the row in its last chunk (a wave's own LDS accesses stay in order)
+        for (int r = lane; r < kRows; r += 64) mine[place(r, end)] = first_bytes(mine[place(r, end)], p.k & 15);
+        __builtin_amdgcn_wave_barrier();
+      }
+      add(0, of_a(mine), of_b(mine));
+    }
+  } else {  // rows at other boundaries, or far apart: straight to registers
+    const uint8_t *a[TM], *b[TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) a[i] = p.a + int64_t(m0 + i * 16 + r16 < p.m ? m0 + i * 16 + r16 : p.m - 1) * p.a_stride + g * 16;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) b[j] = p.b + int64_t(n0 + j * 16 + r16 < p.n ? n0 + j * 16 + r16 : p.n - 1) * p.b_stride + g * 16;
+    for (int block = wave; block < p.blocks; block += WAVES) {
+      const int k0 = block * WDP_BLOCK, left = p.k - k0 - g * 16;
+      i32x4 la[TM][2], lb[TN][2];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) lb[j][0] = load_chunk(b[j], k0, left, p.aligned), lb[j][1] = load_chunk(b[j], k0 + 64, left - 64, p.aligned);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) la[i][0] = load_chunk(a[i], k0, left, p.aligned), la[i][1] = load_chunk(a[i], k0 + 64, left - 64, p.aligned);
+      scales(0, block);
+      add(0, [&](int i) { return fragment<FA, EXACT>(la[i][0], la[i][1]); }, [&](int j) { return fragment<FB, EXACT>(lb[j][0], lb[j][1]); });
+    }
   }
-  for (; block < p.blocks; block += WAVES) {
-    const int k0 = block * WDP_BLOCK, left = p.k - k0 - g * 16;
-#pragma unroll
-    for (int j = 0; j < TN; ++j) lb[0][j][0] = load_chunk(b[j], k0, left, p.aligned), lb[0][j][1] = load_chunk(b[j], k0 + 64, left - 64, p.aligned);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) la[0][i][0] = load_chunk(a[i], k0, left, p.aligned), la[0][i][1] = load_chunk(a[i], k0 + 64, left - 64, p.aligned);
-    scales(0, block);
-    add(0);
-  }
+  f32x4(*sums)[TM][TN][64] = reinterpret_cast<f32x4(*)[TM][TN][64]>(lds);
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -804,11 +855,14 @@ template <int FA, int FB, typename C, int PN, int KB> int launch_panel(ProductAr
 // Which kernel, by sizes and alignment (us on this card; k in blocks of 128).
 //   - Many rows against up to 64 columns and 256 of k: b in LDS.  2000000 x 5 x 64: 38 against 108 in tiles of 64;
 //     300000 x 47 x 200: 26 against 28; 10000 x 5 x 300 would take 8.7 against 5.2, hence the bound on m.
-//   - Up to 128 tiles of 64 x 64 (a launch of tiles would leave half the chip idle through all of k): b streamed, in the
-//     largest piece of c, not above m rows, that still makes 150 workgroups (a CU brings some 27 GB/s, so it takes many).
-//     128 x 4096 x 4096: 15 against 20; 700 x 700 x 3000: 10 against 16; 112 x 2445 x 5638: 16 in pieces of 64 x 32, 22 in
-//     32 x 32, 24 in tiles; beyond, 200 x 4096 x 4096: 28 against 21.  With k of one or two blocks there is nothing to stream:
-//     2000 x 256 x 128 takes 4.0 against 3.2, so only up to 32 tiles there (300 x 200 x 256: 2.8 against 3.6).
+//   - Up to 128 tiles of 64 x 64 (a launch of tiles would leave half the chip idle through all of k): blocks of k dealt to the
+//     waves, in the largest piece of c, not above m rows, that still makes 150 workgroups.  128 x 4096 x 4096: 10.2 in pieces
+//     of 64 x 32, 13.8 in 32 x 16, 17.6 in tiles; 64 x 4096 x 4096: 7.8 in 64 x 16, 8.8 in 32 x 16, 9.4 in 64 x 32; 300 x 300 x
+//     3000: 4.7 in 32 x 16, 6.2 in 64 x 16, 7.4 in 64 x 32; 32 x 8192 x 8192: 15.4 in 32 x 16, 23.9 in 16 x 16; 256 x 256 x 8192:
+//     5.7 in 16 x 16, 8.2 in 64 x 16.  With k of one or two blocks there is nothing to deal: 2000 x 256 x 256 takes 4.0 against
+//     3.4, so only up to 32 tiles there (300 x 200 x 256: 2.8 against 3.6).
+//   - 150 to 256 tiles of 64 x 64 and a long k: the same in pieces of 64 x 64, one a CU.  256 x 4096 x 4096: 15.4 against 17.8;
+//     1024^3: 7.6 against 6.4.
 //   - Rows that do not start at 16-byte boundaries: tiles by way of registers.
 //   - Else the tiles that need the least time for a block of k: rounds of 256 tiles of 256 x 256 at 2.1, 512 of 128 x 128
 //     at 1.2 (1.0 with one tile a CU at most), 1024 of 64 x 64 at 1.5 (0.95, 0.65 with two, one a CU); exact ones 2.0 and
@@ -825,13 +879,14 @@ template <int FA, int FB, typename C> int launch_slice(const ProductArgs& p, hip
   }
   if (t64 <= 128 && (p.blocks > 2 || t64 <= 32)) {
     if (p.m > 32 && tiles(64, 32) >= 150) return launch_stream<FA, FB, C, 4, 2, 8, 1>(p, stream);
-    if (p.m > 16 && tiles(32, 32) >= 150) return launch_stream<FA, FB, C, 2, 2, 8, 2>(p, stream);
-    if (p.m > 16 && tiles(32, 16) >= 150) return launch_stream<FA, FB, C, 2, 1, 8, 2>(p, stream);
-    return launch_stream<FA, FB, C, 1, 1, 8, 4>(p, stream);
+    if (p.m > 32 && tiles(64, 16) >= 150) return launch_stream<FA, FB, C, 4, 1, 8, 1>(p, stream);
+    if (p.m > 16 && tiles(32, 16) >= 150) return launch_stream<FA, FB, C, 2, 1, 8, 1>(p, stream);
+    return launch_stream<FA, FB, C, 1, 1, 8, 2>(p, stream);
   }
-  // (places in a tile are 32-bit offsets from its first row)
-  const bool near = p.a_stride <= (1 << 23) && p.b_stride <= (1 << 23) && p.as_row <= (1 << 27);
-  if (!p.aligned || !near || p.m < 64) return launch_tiles<FA, FB, C, 128, 128, 2, 2>(p, stream);
+  if constexpr (!EXACT) {
+    if (p.staged && p.as_row <= (1 << 23) && p.bs_row <= (1 << 23) && t64 >= 150 && t64 <= 256 && p.blocks >= 16) return launch_stream<FA, FB, C, 4, 4, 8, 1>(p, stream);
+  }
+  if (!p.staged || p.as_row > (1 << 27) || p.m < 64) return launch_tiles<FA, FB, C, 128, 128, 2, 2>(p, stream);
   const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
   double cost64 = t64 <= 256 ? 0.65 : t64 <= 512 ? 0.95 : 1.5 * rounds(t64, 1024);
   const double cost128 = t128 <= 256 ? 1.0 : (EXACT ? 2.0 : 1.17) * rounds(t128, 512), cost256 = 2.1 * rounds(t256, 256);
@@ -902,10 +957,12 @@ int wdp_product(const wdp_product_config* cfg, const wdp_product_buffers* b) {
   if (cfg->m == 0 || cfg->n == 0) return WD_OK;
   if (!b->a || !b->a_scale || !b->b || !b->b_scale || !b->c) return WD_E_NULL;
   if (!aligned(b->a_scale, 4) || !aligned(b->b_scale, 4) || !aligned(b->c, size_of(cfg->c_type)) || !aligned(b->workspace, 256)) return WD_E_ALIGN;
+  // (places in a tile are 32-bit offsets from its first row)
+  const bool in_line = aligned(b->a, 16) && aligned(b->b, 16) && cfg->a_stride % 16 == 0 && cfg->b_stride % 16 == 0;
   const ProductArgs p = {static_cast<const uint8_t*>(b->a), static_cast<const uint8_t*>(b->b), b->a_scale, b->b_scale, b->c, cfg->a_stride, cfg->b_stride,
                          cfg->c_stride, cfg->a_scale_row_stride, cfg->a_scale_block_stride, cfg->b_scale_row_stride, cfg->b_scale_block_stride,
                          int32_t(cfg->m), cfg->n, cfg->k, (cfg->k + WDP_BLOCK - 1) / WDP_BLOCK, 0, 0,
-                         aligned(b->a, 16) && aligned(b->b, 16) && cfg->a_stride % 16 == 0 && cfg->b_stride % 16 == 0, cfg->b_scale_rows == 1};
+                         in_line, in_line && cfg->a_stride <= (1 << 23) && cfg->b_stride <= (1 << 23), cfg->b_scale_rows == 1};
   const hipStream_t stream = static_cast<hipStream_t>(cfg->stream);
   const bool wide_a = cfg->a_type == WDP_E5M2, wide_b = cfg->b_type == WDP_E5M2;
   if (wide_a) return wide_b ? launch_c<1, 1>(p, cfg->c_type, stream) : launch_c<1, 0>(p, cfg->c_type, stream);

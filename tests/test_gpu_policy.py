@@ -885,3 +885,38 @@ def test_product_of_many_blocks_of_k(m, n, k, by_row, a_type, b_type, dtype):
         check_product(a, a_scale, b, far, by_row, wd.product8(wide(a), a_scale, wide(b), far, dtype=dtype))
         del far
         torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("m,n,k", [(130, 4090, 2500), (200, 3300, 2049), (33, 2500, 1000), (20, 2450, 777), (17, 200, 5001), (1, 77, 2047), (300, 300, 2999), (64, 4001, 385), (5, 33, 130)])
+@pytest.mark.parametrize("by_row,dtype", [(False, BF16), (True, F16), (True, F32)])
+def test_product_of_few_rows(m, n, k, by_row, dtype):
+    """NaN codes behind the rows at 16-byte boundaries and at others, a guard around c."""
+    gen = generator(m, n, k)
+    a, a_scale, b, b_scale = operands(gen, m, n, k, by_row=by_row)
+    if dtype == F16:
+        a_scale = a_scale * 0.01
+
+    def wide(t, pitch):
+        store = torch.full((t.shape[0] + 1, k + pitch), 0x7F, dtype=torch.uint8, device=DEV)
+        store[:-1, :k] = t.contiguous().view(torch.uint8)
+        return store.view(t.dtype)[:-1, :k]
+
+    for pitch in (-k % 16 + 16, 1 + k % 2):
+        c = torch.full((m + 1, n + 9), 3.0, device=DEV, dtype=dtype)
+        wd.product8(wide(a, pitch), a_scale, wide(b, pitch), b_scale, out=c[:m, :n])
+        check_product(a, a_scale, b, b_scale, by_row, c[:m, :n])
+        assert (c[m:] == 3).all() and (c[:, n:] == 3).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 40, 300), (20, 17, 1000), (70, 40, 130)])
+def test_product_of_rows_far_apart(m, n, k):
+    gen = generator(m, n, k)
+    a, a_scale, b, b_scale = operands(gen, m, n, k)
+
+    def far(t):
+        out = torch.empty_strided(t.shape, ((1 << 23) + 16, 1), dtype=torch.uint8, device=DEV)
+        out.copy_(t.contiguous().view(torch.uint8))
+        return out.view(t.dtype)
+
+    for dtype in (BF16, F32):
+        check_product(a, a_scale, b, b_scale, False, wd.product8(far(a), a_scale, far(b), b_scale, dtype=dtype))
