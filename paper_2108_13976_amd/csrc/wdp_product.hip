@@ -94,17 +94,25 @@ __device__ __forceinline__ i32x4 first_bytes(i32x4 v, int have) {
 }
 
 // Sixteen bytes of a row at `at`; those from `left` on do not exist and read as zero.  A chunk at a 16-byte boundary that
-// holds a byte of the row can be read whole (no page ends inside it).
+// holds a byte of the row can be read whole (no page ends inside it); of other rows the sixteen bytes up to the end are read and
+// moved (one by one 16 x 1000 x 300 takes 8.1 us, so 3.3).
 __device__ __forceinline__ i32x4 load_chunk(const uint8_t* row, int64_t at, int left, bool aligned) {
   if (left >= 16) return load_raw<i32x4>(row + at);
   if (left <= 0) return i32x4{0, 0, 0, 0};
   if (aligned) return first_bytes(load_raw<i32x4>(row + at), left);
   uint64_t lo = 0, hi = 0;
-#pragma unroll 1
-  for (int i = 0; i < left; ++i) {
-    const uint64_t byte = row[at + i];
-    if (i < 8) lo |= byte << (8 * i);
-    else hi |= byte << (8 * i - 64);
+  if (at + left >= 16) {
+    const i32x4 v = load_raw<i32x4>(row + at + left - 16);
+    const int by = 8 * (16 - left);  // 8 .. 120
+    lo = uint64_t(uint32_t(v[1])) << 32 | uint32_t(v[0]), hi = uint64_t(uint32_t(v[3])) << 32 | uint32_t(v[2]);
+    lo = by < 64 ? lo >> by | hi << (64 - by) : hi >> (by - 64);
+    hi = by < 64 ? hi >> by : 0;
+  } else {  // (a row of fewer than sixteen bytes)
+    for (int i = 0; i < left; ++i) {
+      const uint64_t byte = row[at + i];
+      if (i < 8) lo |= byte << (8 * i);
+      else hi |= byte << (8 * i - 64);
+    }
   }
   return i32x4{int(lo), int(lo >> 32), int(hi), int(hi >> 32)};
 }
@@ -662,7 +670,16 @@ __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs 
       if (kNear) __builtin_amdgcn_sched_barrier(0);  // (a row of operands at a time in the registers)
     }
   };
-  if (kNear || p.staged) {  // by way of the wave's own part of LDS
+  i32x4* mine = lds + wave * (DEPTH * kRows * 8);  // the wave's own part
+  // (place() of sixteen rows further is 128 chunks further)
+  const uint32_t first_a = uint32_t(place(r16, g)), first_b = first_a + 128 * TM;
+  const auto of_a = [&](const i32x4* block) {
+    return [block, at = here(first_a)](int i) { return fragment<FA, EXACT>(block[at + 128 * i], block[(at ^ 4) + 128 * i]); };
+  };
+  const auto of_b = [&](const i32x4* block) {
+    return [block, at = here(first_b)](int j) { return fragment<FB, EXACT>(block[at + 128 * j], block[(at ^ 4) + 128 * j]); };
+  };
+  if (kNear || p.staged) {
     // eights of rows, a lane the chunk of row lane / 8 that belongs at place lane % 8 (odd eights: four further or back)
     const auto chunk_of = [](int lane) { return ((lane & 7) ^ (lane >> 4)) * 16; };
     uint32_t from[2 * (TM + TN)];
@@ -672,15 +689,6 @@ __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs 
       from[i] = uint32_t(r < most ? r : most) * uint32_t(i < 2 * TM ? p.a_stride : p.b_stride) + (chunk_of(lane) ^ (64 * (i & 1)));
     }
     const uint8_t *tile_a = p.a + int64_t(m0) * p.a_stride, *tile_b = p.b + int64_t(n0) * p.b_stride;
-    i32x4* mine = lds + wave * (DEPTH * kRows * 8);
-    // (place() of sixteen rows further is 128 chunks further)
-    const uint32_t first_a = uint32_t(place(r16, g)), first_b = first_a + 128 * TM;
-    const auto of_a = [&](const i32x4* block) {
-      return [block, at = here(first_a)](int i) { return fragment<FA, EXACT>(block[at + 128 * i], block[(at ^ 4) + 128 * i]); };
-    };
-    const auto of_b = [&](const i32x4* block) {
-      return [block, at = here(first_b)](int j) { return fragment<FB, EXACT>(block[at + 128 * j], block[(at ^ 4) + 128 * j]); };
-    };
     const int whole = p.k / WDP_BLOCK;
     for (int block = wave; block < whole; block += DEPTH * WAVES) {
 #pragma unroll
@@ -712,21 +720,22 @@ __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs 
       }
       add(0, of_a(mine), of_b(mine));
     }
-  } else {  // rows at other boundaries, or far apart: straight to registers
-    const uint8_t *a[TM], *b[TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) a[i] = p.a + int64_t(m0 + i * 16 + r16 < p.m ? m0 + i * 16 + r16 : p.m - 1) * p.a_stride + g * 16;
-#pragma unroll
-    for (int j = 0; j < TN; ++j) b[j] = p.b + int64_t(n0 + j * 16 + r16 < p.n ? n0 + j * 16 + r16 : p.n - 1) * p.b_stride + g * 16;
+  } else if constexpr (!kNear) {  // rows at other boundaries, or far apart: the same by way of registers
     for (int block = wave; block < p.blocks; block += WAVES) {
-      const int k0 = block * WDP_BLOCK, left = p.k - k0 - g * 16;
-      i32x4 la[TM][2], lb[TN][2];
+      const int k0 = block * WDP_BLOCK + (lane & 7) * 16;
+      i32x4 chunks[2 * (TM + TN)];
 #pragma unroll
-      for (int j = 0; j < TN; ++j) lb[j][0] = load_chunk(b[j], k0, left, p.aligned), lb[j][1] = load_chunk(b[j], k0 + 64, left - 64, p.aligned);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) la[i][0] = load_chunk(a[i], k0, left, p.aligned), la[i][1] = load_chunk(a[i], k0 + 64, left - 64, p.aligned);
+      for (int i = 0; i < 2 * (TM + TN); ++i) {
+        const int r = (i < 2 * TM ? i : i - 2 * TM) * 8 + (lane >> 3);
+        const uint8_t* row = i < 2 * TM ? p.a + int64_t(m0 + r < p.m ? m0 + r : p.m - 1) * p.a_stride : p.b + int64_t(n0 + r < p.n ? n0 + r : p.n - 1) * p.b_stride;
+        chunks[i] = load_chunk(row, k0, p.k - k0, p.aligned);
+      }
       scales(0, block);
-      add(0, [&](int i) { return fragment<FA, EXACT>(la[i][0], la[i][1]); }, [&](int j) { return fragment<FB, EXACT>(lb[j][0], lb[j][1]); });
+#pragma unroll
+      for (int i = 0; i < 2 * (TM + TN); ++i) mine[place(i * 8 + (lane >> 3), lane & 7)] = chunks[i];
+      __builtin_amdgcn_wave_barrier();  // (a wave's own LDS accesses stay in order)
+      add(0, of_a(mine), of_b(mine));
+      __builtin_amdgcn_wave_barrier();
     }
   }
   f32x4(*sums)[TM][TN][64] = reinterpret_cast<f32x4(*)[TM][TN][64]>(lds);

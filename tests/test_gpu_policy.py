@@ -920,3 +920,21 @@ def test_product_of_rows_far_apart(m, n, k):
 
     for dtype in (BF16, F32):
         check_product(a, a_scale, b, b_scale, False, wd.product8(far(a), a_scale, far(b), b_scale, dtype=dtype))
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 33, 7), (3, 17, 15), (20000, 9, 13), (200, 300, 5), (20000, 40, 200), (600, 700, 1001), (1000, 1000, 129)])
+@pytest.mark.parametrize("pitch", [0, 1, 2])
+def test_product_of_rows_at_odd_addresses(m, n, k, pitch):
+    """Rows one behind the other, NaN codes in front of the first and behind the last."""
+    gen = generator(m, n, k, 3)
+    a, a_scale, b, b_scale = operands(gen, m, n, k)
+
+    def at_odd(t):
+        rows = t.shape[0]
+        store = torch.full((1 + rows * (k + pitch) + 16,), 0x7F, dtype=torch.uint8, device=DEV)
+        out = store[1:1 + rows * (k + pitch)].view(rows, k + pitch)[:, :k]
+        out.copy_(t.contiguous().view(torch.uint8))
+        return out.view(t.dtype)
+
+    for dtype in (BF16, F32):
+        check_product(a, a_scale, b, b_scale, False, wd.product8(at_odd(a), a_scale, at_odd(b), b_scale, dtype=dtype))
