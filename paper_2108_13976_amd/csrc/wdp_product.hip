@@ -874,8 +874,9 @@ template <int FA, int FB, typename C, int PN, int KB> int launch_panel(ProductAr
 //     1024^3: 7.6 against 6.4.
 //   - Rows that do not start at 16-byte boundaries: tiles by way of registers.
 //   - Else the tiles that need the least time for a block of k: rounds of 256 tiles of 256 x 256 at 2.1, 512 of 128 x 128
-//     at 1.2 (1.0 with one tile a CU at most), 1024 of 64 x 64 at 1.5 (0.95, 0.65 with two, one a CU); exact ones 2.0 and
-//     1.5.  4096^3: 67 against 75 and (64) 100; 2048 x 2048 x 2000: 35, 19, 25; 1000^3: 19, 10.5, 8.3.  Columns up to 64
+//     at 1.2 (1.0 with one tile a CU at most), 1024 of 64 x 64 at 1.5 (0.95, 0.65 with three, one a CU); exact ones 2.0 and
+//     1.5.  4096^3: 67 against 75 and (64) 100; 2048 x 2048 x 2000: 35, 19, 25; 1000^3: 19, 10.5, 8.3;
+//     1500 x 1500 x 2000 with a scale a column: 128 19, 64 15.5, 2000 x 2000 x 2000: 18.6, 22.8.  Columns up to 64
 //     leave half of a wider tile empty: 500000 x 64 x 300 takes 58 against 50.
 template <int FA, int FB, typename C> int launch_slice(const ProductArgs& p, hipStream_t stream) {
   constexpr bool EXACT = sizeof(C) == 4;
@@ -897,7 +898,7 @@ template <int FA, int FB, typename C> int launch_slice(const ProductArgs& p, hip
   }
   if (!p.staged || p.as_row > (1 << 27) || p.m < 64) return launch_tiles<FA, FB, C, 128, 128, 2, 2>(p, stream);
   const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
-  double cost64 = t64 <= 256 ? 0.65 : t64 <= 512 ? 0.95 : 1.5 * rounds(t64, 1024);
+  double cost64 = t64 <= 256 ? 0.65 : t64 <= 768 ? 0.95 : 1.5 * rounds(t64, 1024);
   const double cost128 = t128 <= 256 ? 1.0 : (EXACT ? 2.0 : 1.17) * rounds(t128, 512), cost256 = 2.1 * rounds(t256, 256);
   if (p.n <= 64) cost64 = 0.0;
   if constexpr (!EXACT) {
