@@ -938,3 +938,22 @@ def test_product_of_rows_at_odd_addresses(m, n, k, pitch):
 
     for dtype in (BF16, F32):
         check_product(a, a_scale, b, b_scale, False, wd.product8(at_odd(a), a_scale, at_odd(b), b_scale, dtype=dtype))
+
+
+@pytest.mark.parametrize("rows,width", [(1, 1), (70000, 3), (70001, 8), (50000, 9), (40003, 16), (600001, 7), (600000, 13)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_norm_of_very_short_rows(rows, width, dtype):
+    """One or two lanes a row: outputs, gradients; dw's terms are added in chains of at most rows / 8 and 20 levels."""
+    gen = generator(rows, width)
+    x, w, r, dy = normal(gen, rows, width, dtype=dtype), 1 + 0.1 * normal(gen, width), normal(gen, rows, width, dtype=dtype), normal(gen, rows, width, dtype=dtype)
+    out = wd.rms_norm(x, w, residual=r, out8=E4M3, y=True)
+    check_norm(x, w, r, 1e-5, out, E4M3)
+    dx, dw = wd.rms_norm_backward(dy, out.h, w, out.rstd)
+    xhat = ref.f64(out.h) * ref.f64(out.rstd)[:, None]
+    terms = ref.f64(dy) * xhat
+    assert ((ref.f64(dw) - terms.sum(0)).abs() <= (rows / 8 + 24) * EPS24 * terms.abs().sum(0)).all()
+    g = ref.f64(dy) * ref.f64(w)
+    mean = (g * xhat).mean(1, keepdim=True)
+    want = ref.f64(out.rstd)[:, None] * (g - xhat * mean)
+    size = ref.f64(out.rstd)[:, None] * (g.abs() + xhat.abs() * (g * xhat).abs().mean(1, keepdim=True))
+    assert ((ref.f64(dx) - want).abs() <= (width + 24) * EPS24 * size + ref.rounding(want, dtype) * 1.01 + 1e-36).all()
