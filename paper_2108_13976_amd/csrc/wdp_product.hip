@@ -606,20 +606,21 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_long_kernel(ProductAr
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------
-// A workgroup owns 16 TM rows and 16 TN columns, its waves take the blocks of k in turn, DEPTH of them requested at a time,
-// and join their sums in LDS.  No barrier before that: a wave waits for its own requests alone, the other seven's are under
+// A workgroup owns 16 TM rows and 16 TN columns, its waves take the blocks of k in turn and join their sums
+// in LDS.  No barrier before that: a wave waits for its own requests alone, the other seven's are under
 // way meanwhile.
 //
 // A block's rows go through LDS though each is read once: an instruction's operand has sixteen rows in sixteen neighbouring
 // lanes, and requests in that order, sixteen bytes of sixteen lines, reach 38 GB/s a CU; eight lanes to a line reach 90 to
 // 110 (both from L2).  Straight to registers 112 x 2448 x 5632 took 18.7 us (here 11.5), 256 x 256 x 8192 9.7 (5.7),
-// 16 x 4096 x 4096 6.3 (4.8), with four blocks under way as with one.
-template <int FA, int FB, typename C, int TM, int TN, int WAVES, int DEPTH>
+// 16 x 4096 x 4096 6.3 (4.8).  A wave has one block under way: with two, more LDS and fewer workgroups a CU, 1 x 50000 x 1024
+// takes 17.2 us and not 13.7, 16 x 4096 x 4096 from memory 6.3 and not 5.9.
+template <int FA, int FB, typename C, int TM, int TN, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs p) {
   constexpr bool EXACT = sizeof(C) == 4;
   constexpr int kRows = 16 * (TM + TN);    // of a staged block: those of a, then of b
   constexpr bool kNear = TM * TN >= 16;    // (the largest piece is taken for near rows and scales alone: 32-bit places)
-  __shared__ i32x4 lds[WAVES * DEPTH * kRows * 8];
+  __shared__ i32x4 lds[WAVES * kRows * 8];
   static_assert(sizeof(lds) >= WAVES * TM * TN * sizeof(f32x4) * 64, "sums are joined there");
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r16 = lane & 15, g = lane >> 4;
   const int n0 = blockIdx.x * 16 * TN, m0 = blockIdx.y * 16 * TM;
@@ -643,41 +644,36 @@ __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs 
     bs[j] = Place(p.by_row ? at - n0 : at / WDP_BLOCK - n0 / WDP_BLOCK) * b_pitch;
     more[j] = p.n - 1 - at;
   }
-  float sa[DEPTH][TM], sb[DEPTH][TN][4];
-  auto scales = [&](int d, int block) {
+  float sa[TM], sb[TN][4];
+  auto scales = [&](int block) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sa[d][i] = scale_at(tile_as + block * p.as_block, as[i]);
+    for (int i = 0; i < TM; ++i) sa[i] = scale_at(tile_as + block * p.as_block, as[i]);
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      sb[d][j][0] = scale_at(tile_bs + block * p.bs_block, bs[j]);
+      sb[j][0] = scale_at(tile_bs + block * p.bs_block, bs[j]);
 #pragma unroll
-      for (int e = 1; e < 4; ++e) sb[d][j][e] = p.by_row ? scale_at(tile_bs + block * p.bs_block, bs[j] + Place(e < more[j] ? e : more[j]) * b_pitch) : sb[d][j][0];
+      for (int e = 1; e < 4; ++e) sb[j][e] = p.by_row ? scale_at(tile_bs + block * p.bs_block, bs[j] + Place(e < more[j] ? e : more[j]) * b_pitch) : sb[j][0];
     }
   };
-  auto add = [&](int d, auto row_of_a, auto row_of_b) {
+  i32x4* mine = lds + wave * (kRows * 8);  // the wave's own part
+  // (place() of sixteen rows further is 128 chunks further)
+  const uint32_t first_a = uint32_t(place(r16, g)), first_b = first_a + 128 * TM;
+  auto add = [&]() {
+    const uint32_t at_a = here(first_a), at_b = here(first_b);
     Fragment<EXACT> fb[TN];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) fb[j] = row_of_b(j);
+    for (int j = 0; j < TN; ++j) fb[j] = fragment<FB, EXACT>(mine[at_b + 128 * j], mine[(at_b ^ 4) + 128 * j]);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const Fragment<EXACT> fa = row_of_a(i);
+      const Fragment<EXACT> fa = fragment<FA, EXACT>(mine[at_a + 128 * i], mine[(at_a ^ 4) + 128 * i]);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         const f32x4 part = inner<FA, FB, EXACT>(fb[j], fa);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[e], sa[d][i] * sb[d][j][e], acc[i][j][e]);
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[e], sa[i] * sb[j][e], acc[i][j][e]);
       }
       if (kNear) __builtin_amdgcn_sched_barrier(0);  // (a row of operands at a time in the registers)
     }
-  };
-  i32x4* mine = lds + wave * (DEPTH * kRows * 8);  // the wave's own part
-  // (place() of sixteen rows further is 128 chunks further)
-  const uint32_t first_a = uint32_t(place(r16, g)), first_b = first_a + 128 * TM;
-  const auto of_a = [&](const i32x4* block) {
-    return [block, at = here(first_a)](int i) { return fragment<FA, EXACT>(block[at + 128 * i], block[(at ^ 4) + 128 * i]); };
-  };
-  const auto of_b = [&](const i32x4* block) {
-    return [block, at = here(first_b)](int j) { return fragment<FB, EXACT>(block[at + 128 * j], block[(at ^ 4) + 128 * j]); };
   };
   if (kNear || p.staged) {
     // eights of rows, a lane the chunk of row lane / 8 that belongs at place lane % 8 (odd eights: four further or back)
@@ -690,21 +686,12 @@ __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs 
     }
     const uint8_t *tile_a = p.a + int64_t(m0) * p.a_stride, *tile_b = p.b + int64_t(n0) * p.b_stride;
     const int whole = p.k / WDP_BLOCK;
-    for (int block = wave; block < whole; block += DEPTH * WAVES) {
+    for (int block = wave; block < whole; block += WAVES) {
 #pragma unroll
-      for (int d = 0; d < DEPTH; ++d) {
-        const int at = block + d * WAVES;
-        if (d > 0 && at >= whole) break;
-#pragma unroll
-        for (int i = 0; i < 2 * (TM + TN); ++i) to_lds((i < 2 * TM ? tile_a : tile_b) + at * WDP_BLOCK + here(from[i]), mine + (d * kRows + i * 8) * 8);
-        scales(d, at);
-      }
+      for (int i = 0; i < 2 * (TM + TN); ++i) to_lds((i < 2 * TM ? tile_a : tile_b) + block * WDP_BLOCK + here(from[i]), mine + i * 64);
+      scales(block);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the wave's own requests: no other wave reads them)
-#pragma unroll
-      for (int d = 0; d < DEPTH; ++d) {
-        if (d > 0 && block + d * WAVES >= whole) break;
-        add(d, of_a(mine + d * kRows * 8), of_b(mine + d * kRows * 8));
-      }
+      add();
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (read before the next requests may write there)
     }
     if (whole < p.blocks && wave == whole % WAVES) {  // what is left of k
@@ -712,13 +699,13 @@ __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs 
 #pragma unroll
       for (int i = 0; i < 2 * (TM + TN); ++i)  // zeros in place of chunks with nothing of the row,
         to_lds(k0 + (chunk ^ (64 * (i & 1))) < p.k ? (i < 2 * TM ? tile_a : tile_b) + k0 + here(from[i]) : reinterpret_cast<const uint8_t*>(&kZeros), mine + i * 64);
-      scales(0, whole);
+      scales(whole);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       if (p.k & 15) {  // and of the bytes behind the row in its last chunk (a wave's own LDS accesses stay in order)
         for (int r = lane; r < kRows; r += 64) mine[place(r, end)] = first_bytes(mine[place(r, end)], p.k & 15);
         __builtin_amdgcn_wave_barrier();
       }
-      add(0, of_a(mine), of_b(mine));
+      add();
     }
   } else if constexpr (!kNear) {  // rows at other boundaries, or far apart: the same by way of registers
     for (int block = wave; block < p.blocks; block += WAVES) {
@@ -730,11 +717,11 @@ __global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs 
         const uint8_t* row = i < 2 * TM ? p.a + int64_t(m0 + r < p.m ? m0 + r : p.m - 1) * p.a_stride : p.b + int64_t(n0 + r < p.n ? n0 + r : p.n - 1) * p.b_stride;
         chunks[i] = load_chunk(row, k0, p.k - k0, p.aligned);
       }
-      scales(0, block);
+      scales(block);
 #pragma unroll
       for (int i = 0; i < 2 * (TM + TN); ++i) mine[place(i * 8 + (lane >> 3), lane & 7)] = chunks[i];
       __builtin_amdgcn_wave_barrier();  // (a wave's own LDS accesses stay in order)
-      add(0, of_a(mine), of_b(mine));
+      add();
       __builtin_amdgcn_wave_barrier();
     }
   }
@@ -851,8 +838,8 @@ template <int FA, int FB, bool ROWS, typename C, int BM, int BN, int WM, int WN>
   p.n_tiles = (p.n + BN - 1) / BN;
   return enqueue(product_long_kernel<FA, FB, ROWS, C, BM, BN, WM, WN>, dim3(unsigned(p.m_tiles) * unsigned(p.n_tiles)), 64 * WM * WN, stream, p);
 }
-template <int FA, int FB, typename C, int TM, int TN, int WAVES, int DEPTH> int launch_stream(const ProductArgs& p, hipStream_t stream) {
-  return enqueue(product_stream_kernel<FA, FB, C, TM, TN, WAVES, DEPTH>,
+template <int FA, int FB, typename C, int TM, int TN, int WAVES> int launch_stream(const ProductArgs& p, hipStream_t stream) {
+  return enqueue(product_stream_kernel<FA, FB, C, TM, TN, WAVES>,
                  dim3(unsigned((p.n + 16 * TN - 1) / (16 * TN)), unsigned((p.m + 16 * TM - 1) / (16 * TM))), 64 * WAVES, stream, p);
 }
 template <int FA, int FB, typename C, int PN, int KB> int launch_panel(ProductArgs p, hipStream_t stream) {
@@ -870,6 +857,9 @@ template <int FA, int FB, typename C, int PN, int KB> int launch_panel(ProductAr
 //     3000: 4.7 in 32 x 16, 6.2 in 64 x 16, 7.4 in 64 x 32; 32 x 8192 x 8192: 15.4 in 32 x 16, 23.9 in 16 x 16; 256 x 256 x 8192:
 //     5.7 in 16 x 16, 8.2 in 64 x 16.  With k of one or two blocks there is nothing to deal: 2000 x 256 x 256 takes 4.0 against
 //     3.4, so only up to 32 tiles there (300 x 200 x 256: 2.8 against 3.6).
+//     Fewer rows than a tile's 64 have no other tiles than 128 x 128 by way of registers: the same up to 16384 columns, beyond
+//     for 16 rows or float32 results and a k of eight blocks.  16 x 16384 x 4096: 17.0 against 22.1 (float32 18 against 102),
+//     60 x 16384 x 1024: 10.1, 14.5; 1 x 50000 x 1024: 13.7, 18.1; but 48 x 50000 x 1024: 31.6, 19.8; 16 x 50000 x 384: 9.7, 8.9.
 //   - 150 to 256 tiles of 64 x 64 and a long k: the same in pieces of 64 x 64, one a CU.  256 x 4096 x 4096: 15.4 against 17.8;
 //     1024^3: 7.6 against 6.4.
 //   - Rows that do not start at 16-byte boundaries: tiles by way of registers.
@@ -887,14 +877,15 @@ template <int FA, int FB, typename C> int launch_slice(const ProductArgs& p, hip
     if (p.blocks == 1) return launch_panel<FA, FB, C, 64, 1>(p, stream);
     return launch_panel<FA, FB, C, 64, 2>(p, stream);
   }
-  if (t64 <= 128 && (p.blocks > 2 || t64 <= 32)) {
-    if (p.m > 32 && tiles(64, 32) >= 150) return launch_stream<FA, FB, C, 4, 2, 8, 1>(p, stream);
-    if (p.m > 32 && tiles(64, 16) >= 150) return launch_stream<FA, FB, C, 4, 1, 8, 1>(p, stream);
-    if (p.m > 16 && tiles(32, 16) >= 150) return launch_stream<FA, FB, C, 2, 1, 8, 1>(p, stream);
-    return launch_stream<FA, FB, C, 1, 1, 8, 2>(p, stream);
+  const bool few = p.m < 64 && (t64 <= 256 || (p.blocks >= 8 && (EXACT || p.m <= 16)));
+  if (((t64 <= 128 || few) && p.blocks > 2) || t64 <= 32) {
+    if (p.m > 32 && tiles(64, 32) >= 150) return launch_stream<FA, FB, C, 4, 2, 8>(p, stream);
+    if (p.m > 32 && tiles(64, 16) >= 150) return launch_stream<FA, FB, C, 4, 1, 8>(p, stream);
+    if (p.m > 16 && tiles(32, 16) >= 150) return launch_stream<FA, FB, C, 2, 1, 8>(p, stream);
+    return launch_stream<FA, FB, C, 1, 1, 8>(p, stream);
   }
   if constexpr (!EXACT) {
-    if (p.staged && p.as_row <= (1 << 23) && p.bs_row <= (1 << 23) && t64 >= 150 && t64 <= 256 && p.blocks >= 16) return launch_stream<FA, FB, C, 4, 4, 8, 1>(p, stream);
+    if (p.staged && p.as_row <= (1 << 23) && p.bs_row <= (1 << 23) && t64 >= 150 && t64 <= 256 && p.blocks >= 16) return launch_stream<FA, FB, C, 4, 4, 8>(p, stream);
   }
   if (!p.staged || p.as_row > (1 << 27) || p.m < 64) return launch_tiles<FA, FB, C, 128, 128, 2, 2>(p, stream);
   const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);

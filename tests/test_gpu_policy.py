@@ -887,7 +887,7 @@ def test_product_of_many_blocks_of_k(m, n, k, by_row, a_type, b_type, dtype):
         torch.cuda.empty_cache()
 
 
-@pytest.mark.parametrize("m,n,k", [(130, 4090, 2500), (200, 3300, 2049), (33, 2500, 1000), (20, 2450, 777), (17, 200, 5001), (1, 77, 2047), (300, 300, 2999), (64, 4001, 385), (5, 33, 130)])
+@pytest.mark.parametrize("m,n,k", [(130, 4090, 2500), (200, 3300, 2049), (33, 2500, 1000), (20, 2450, 777), (17, 200, 5001), (1, 77, 2047), (300, 300, 2999), (64, 4001, 385), (5, 33, 130), (3, 9000, 700), (50, 9001, 400), (2, 17000, 1030)])
 @pytest.mark.parametrize("by_row,dtype", [(False, BF16), (True, F16), (True, F32)])
 def test_product_of_few_rows(m, n, k, by_row, dtype):
     """NaN codes behind the rows at 16-byte boundaries and at others, a guard around c."""
